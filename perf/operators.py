@@ -1,0 +1,661 @@
+"""Operators of one training step around the stage, as cases that can be timed.
+
+A program that trains a decoder next to an encoder, or goes on training one from preferences or rewards, puts these
+between the calls it makes already: rotary positions between the QKV product and the attention, attention over an
+encoder's states, a policy or preference loss behind the head, and AdamW over the parameter tensors.
+
+`own` false: the operators in elementary torch operations.  `own` true: the framework's calls.
+"""
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda:0"
+BLOCK = 256                                   # elements that share a scale where moments are held in 8 bits
+E4M3_MAX = 448.0
+M32 = 0xFFFFFFFF
+
+
+def _lib():
+    from paper_2204_12013_amd import binding
+    return binding
+
+
+# ------------------------------------------------------------------------------------------- cases
+
+def _rotary(name, dtype, T, seq, heads, d, rot, extra, layout, scaling, inverse, in_place, far, base=10000.0, factor=8.0):
+    """extra: columns behind the rotated heads in a row (the values of a packed qkv, or the gap of a strided view)."""
+    return {"name": name, "op": "rotary", "dtype": dtype, "T": T, "seq": seq, "heads": heads, "d": d, "rot": rot,
+            "extra": extra, "layout": layout, "scaling": scaling, "inverse": inverse, "in_place": in_place, "far": far,
+            "base": base, "factor": factor}
+
+
+def _cross(name, dtype, batch, sq, sk, heads, kv_heads, d, lengths, step):
+    return {"name": name, "op": "cross", "dtype": dtype, "batch": batch, "sq": sq, "sk": sk, "heads": heads,
+            "kv_heads": kv_heads, "d": d, "lengths": lengths, "step": step}
+
+
+def _policy(name, dtype, T, V, gap, counted, ref, ent):
+    """gap: columns behind the vocabulary in a row of the logits; counted: share of the tokens that count."""
+    return {"name": name, "op": "policy", "dtype": dtype, "T": T, "V": V, "gap": gap, "counted": counted, "ref": ref,
+            "ent": ent}
+
+
+def _preference(name, dtype, pairs, seq, V, gap, smoothing):
+    return {"name": name, "op": "preference", "dtype": dtype, "pairs": pairs, "seq": seq, "V": V, "gap": gap,
+            "smoothing": smoothing}
+
+
+def _adamw(name, dtype, bits, kind, layers, hidden, packed, sizes_seed=0):
+    """kind "layers": the parameter tensors of that many transformer layers; "mixed": that many tensors of any size up to
+    hidden^2.  packed: the tensors follow each other without gaps, whatever their alignment."""
+    return {"name": name, "op": "adamw", "dtype": dtype, "bits": bits, "kind": kind, "layers": layers, "hidden": hidden,
+            "packed": packed, "sizes_seed": sizes_seed}
+
+
+def listed():
+    return [
+        # one new token of each of eight sequences, far into a long context: queries and keys of its qkv, in place
+        _rotary("rotary_one_token", "bf16", 8, 1, 32, 64, 64, 16 * 64, "halves", "linear", False, True, True),
+        # the backward through the positions of the widest layers: half of each head, neighbours as pairs, a stretched context
+        _rotary("rotary_wide_backward", "bf16", 2048, 2048, 192, 128, 64, 96 * 128, "neighbours", "parts", True, False, False,
+                500000.0),
+        # the fp32 configuration's layer with an encoder in front: a handful of tokens, latency only
+        _cross("cross_tiny_f32", "f32", 2, 16, 24, 2, 2, 32, "full", True),
+        # answering: one query row per sample over long encoder states, padded to the longest, key heads shared by four
+        _cross("cross_one_token", "bf16", 8, 1, 4096, 16, 4, 64, "ragged", False),
+        # a training step of BERT-large sized layers, encoder states cut to their real lengths
+        _cross("cross_ragged_step", "bf16", 8, 512, 333, 16, 16, 64, "ragged", True),
+        # a training step of the widest layers, twelve query heads to a key head
+        _cross("cross_wide_step", "bf16", 1, 2048, 4096, 96, 8, 128, "full", True),
+        # a few answers' tokens in fp32 with a vocabulary that divides by nothing, no reference model
+        _policy("policy_few_f32", "f32", 48, 32003, 0, 0.8, False, 0.0),
+        # a micro-batch of the decoder stage: KL to a reference model and an entropy term, prompts left out
+        _policy("policy_decoder", "bf16", 4096, 50304, 0, 0.75, True, 0.01),
+        # two pairs of short answers
+        _preference("preference_short", "bf16", 2, 24, 50257, 0, 0.0),
+        # four pairs of the encoder's sequence length, smoothed labels
+        _preference("preference_long", "bf16", 4, 512, 30528, 0, 0.1),
+        # the closing step of an iteration of the BERT-large stage: 72 tensors, vectors without decay
+        _adamw("adamw_layers", "bf16", 32, "layers", 6, 1024, False),
+        # the decoder stage with its moments in 8 bits
+        _adamw("adamw_8bit", "bf16", 8, "layers", 6, 1600, False),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(lo * (hi / lo) ** rng.random()))
+
+
+def draw(rng):
+    while True:
+        op = rng.choice(["rotary", "cross", "cross", "policy", "preference", "adamw"])
+        dtype = rng.choice(["bf16", "bf16", "bf16", "f32"])
+        if op == "rotary":
+            d = rng.choice([64, 64, 128, 2 * rng.randint(8, 64)])
+            rot = d if rng.random() < 0.5 else 2 * rng.randint(1, d // 2)
+            scaling = rng.choice(["none", "linear", "stretched", "parts"])
+            seq = _log_int(rng, 1, 8192)
+            # scaled vectors are not written over themselves: a program that repeats the call would grow them
+            c = _rotary("", dtype, seq * _log_int(rng, 1, 16), seq, _log_int(rng, 1, 192), d, rot,
+                        rng.choice([0, d * rng.randint(1, 32), rng.randint(1, 64)]), rng.choice(["halves", "neighbours"]),
+                        scaling, rng.random() < 0.4, scaling != "parts" and rng.random() < 0.5, rng.random() < 0.5,
+                        rng.choice([10000.0, 500000.0]), rng.choice([2.0, 8.0, 32.0]))
+        elif op == "cross":
+            kv_heads, group = _log_int(rng, 1, 16), rng.choice([1, 1, 2, 4, 8])
+            d = rng.choice([64, 64, 128, 128, rng.randint(1, 128)])
+            sq = rng.randint(1, 4) if rng.random() < 0.3 else _log_int(rng, 1, 2048)
+            c = _cross("", dtype, _log_int(rng, 1, 16), sq, _log_int(rng, 1, 8192), kv_heads * group, kv_heads, d,
+                       rng.choice(["full", "ragged"]), rng.random() < 0.6)
+        elif op == "policy":
+            c = _policy("", dtype, _log_int(rng, 1, 4096), _log_int(rng, 100, 131072), rng.choice([0, 0, rng.randint(1, 64)]),
+                        rng.choice([1.0, 0.75, 0.3]), rng.random() < 0.6, rng.choice([0.0, 0.01]))
+        elif op == "preference":
+            c = _preference("", dtype, _log_int(rng, 1, 16), _log_int(rng, 1, 1024), _log_int(rng, 100, 131072),
+                            rng.choice([0, 0, rng.randint(1, 64)]), rng.choice([0.0, 0.1]))
+        else:
+            kind = rng.choice(["layers", "mixed"])
+            c = _adamw("", dtype, rng.choice([8, 32]), kind, _log_int(rng, 1, 6) if kind == "layers" else _log_int(rng, 1, 200),
+                       8 * _log_int(rng, 8, 192) if kind == "layers" else _log_int(rng, 16, 2048), rng.random() < 0.5,
+                       rng.randint(1, 1 << 20))
+        del c["name"]
+        w = work(c)
+        scores = c["batch"] * c["heads"] * c["sq"] * c["sk"] if op == "cross" else 0
+        if w["bytes"] <= 1.2e9 and w["flops"] <= 4e11 and scores <= 4e8:
+            return c
+
+
+# ------------------------------------------------------------------------------------------- inputs
+
+def _act(case):
+    return torch.bfloat16 if case["dtype"] == "bf16" else torch.float32
+
+
+def _frequencies(case):
+    """Angle per position of each pair, in 64 bits, and the factor on the rotated vectors."""
+    rot, base, factor = case["rot"], case["base"], case["factor"]
+    i = torch.arange(rot // 2, dtype=torch.float64)
+    amplitude = 1.0
+    if case["scaling"] == "stretched" and rot > 2:
+        base = base * factor ** (rot / (rot - 2))
+    f = base ** (-2 * i / rot)
+    if case["scaling"] == "linear":
+        f = f / factor
+    if case["scaling"] == "parts":
+        turns = 4096 * f / (2 * math.pi)
+        keep = ((turns - 1) / (32 - 1)).clamp(0, 1)
+        f = f * (keep + (1 - keep) / factor)
+        amplitude = 0.1 * math.log(factor) + 1
+    return f.to(DEV), amplitude
+
+
+def _sizes(case):
+    """(elements, decays) of each tensor."""
+    if case["kind"] == "layers":
+        H, F = case["hidden"], 4 * case["hidden"]
+        one = [(3 * H * H, True), (3 * H, False), (H * H, True), (H, False), (H, False), (H, False), (H * F, True), (F, False),
+               (F * H, True), (H, False), (H, False), (H, False)]
+        return one * case["layers"]
+    g = torch.Generator()
+    g.manual_seed(case["sizes_seed"])
+    top = 2 * math.log(case["hidden"])
+    return [(max(1, int(math.exp(u * top))), u > 0.5) for u in torch.rand(case["layers"], generator=g).tolist()]
+
+
+def _cut(total, sizes, packed, step):
+    """Start of each tensor in a flat buffer, and the buffer's length."""
+    at, starts = 0, []
+    for n in sizes:
+        starts.append(at)
+        at += n if packed else -(-n // step) * step
+    return starts, at
+
+
+def _log_p(logits, labels):
+    z = logits.float()
+    return z.gather(1, labels.long()[:, None])[:, 0] - torch.logsumexp(z, 1)
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    act, op = _act(case), case["op"]
+
+    def normal(*shape):
+        return torch.randn(*shape, generator=gen, device=DEV)
+
+    def uniform(*shape):
+        return torch.rand(*shape, generator=gen, device=DEV)
+    s = {"case": case}
+    if op == "rotary":
+        T, width = case["T"], case["heads"] * case["d"]
+        s["x"] = normal(T, width + case["extra"]).to(act)
+        s["freq"], s["amplitude"] = _frequencies(case)
+        s["pos"] = None
+        if case["far"]:          # positions of their own: new tokens of sequences of any length
+            s["pos"] = (uniform(T) * 1e6).to(torch.int32)
+        s["y"] = s["x"][:, :width] if case["in_place"] else torch.empty(T, width, dtype=act, device=DEV)
+    elif op == "cross":
+        b, sq, sk, d = case["batch"], case["sq"], case["sk"], case["d"]
+        H, Hkv = case["heads"] * d, case["kv_heads"] * d
+        s["q"] = (normal(b * sq, H) * 1.5).to(act)
+        s["kv"] = normal(b * sk, 2 * Hkv).to(act)
+        s["len"] = None
+        if case["lengths"] == "ragged":      # the longest is whole; a short one may be empty
+            n = (uniform(b) * (sk + 1)).to(torch.int32).clamp_(max=sk)
+            n[0] = sk
+            s["len"] = n
+        s["ctx"], s["lse"] = torch.empty(b * sq, H, dtype=act, device=DEV), torch.empty(b, case["heads"], sq, device=DEV)
+        if case["step"]:
+            s["dctx"] = (normal(b * sq, H) / (b * sq * H) ** 0.5).to(act)
+            s["dq"], s["dkv"] = torch.empty_like(s["q"]), torch.empty_like(s["kv"])
+    elif op in ("policy", "preference"):
+        V = case["V"]
+        T = case["T"] if op == "policy" else 2 * case["pairs"] * case["seq"]
+        rows = torch.empty(T, V + case["gap"], dtype=act, device=DEV)
+        s["logits"], s["dlogits"] = rows[:, :V], torch.empty(T, V, dtype=act, device=DEV)
+        labels = []
+        for t in range(0, T, 512):           # answers that the model itself gave: labels drawn from its distribution
+            z = normal(min(512, T - t), V) * 2.5
+            rows[t:t + 512, :V] = z.to(act)
+            labels.append((z - uniform(*z.shape).clamp_(1e-20, 1 - 1e-7).log_().neg_().log_()).argmax(1))
+        s["labels"] = torch.cat(labels).to(torch.int32)
+        s["logp"] = torch.empty(T, device=DEV)
+        now = torch.cat([_log_p(s["logits"][t:t + 512], s["labels"][t:t + 512]) for t in range(0, T, 512)])
+        if op == "policy":
+            s["mask"] = None if case["counted"] == 1.0 else (uniform(T) < case["counted"]).to(torch.uint8)
+            s["old"], s["adv"] = now + 0.1 * normal(T), normal(T)
+            s["ref"] = now + 0.3 * normal(T) if case["ref"] else None
+            s["scale"] = 1.0 / max(1.0, T * case["counted"])
+            s["loss"], s["kl"], s["ent"] = (torch.empty(T, device=DEV) for _ in range(3))
+        else:
+            n, S = 2 * case["pairs"], case["seq"]
+            # answers end at lengths of their own, prompts in front of them do not count
+            first = (uniform(n, 1) * S * 0.3).long()
+            last = first + 1 + (uniform(n, 1) * (S - first)).long()
+            t = torch.arange(S, device=DEV)[None]
+            s["mask"] = ((t >= first) & (t < last)).to(torch.uint8).reshape(-1)
+            s["ref"] = ((now + 0.3 * normal(T)) * s["mask"]).view(n, S).double().sum(1).float()
+            s["lse"], s["logp_seq"], s["loss"] = (torch.empty(k, device=DEV) for k in (T, n, case["pairs"]))
+    else:
+        sizes = _sizes(case)
+        n = [k for k, _ in sizes]
+        starts, total = _cut(0, n, case["packed"], 64)
+        blocks = [-(-k // BLOCK) for k in n]
+        bstarts, btotal = _cut(0, blocks, True, 1)
+        size = 1e-3 * torch.exp(normal(total))
+
+        def views(t, at, count):
+            return [t[a:a + k] for a, k in zip(at, count)]
+        s["flat"] = flat = {"g": normal(total) * size, "master": normal(total) * 0.02}
+        flat["w"] = flat["master"].to(act)
+        m, v = 0.3 * normal(total) * size, (size * (0.5 + uniform(total))).square()
+        if case["bits"] == 32:
+            flat["m"], flat["v"] = m, v
+        else:
+            for name, x in (("m", m), ("v", v.sqrt())):
+                code = torch.zeros(total, dtype=torch.float8_e4m3fn, device=DEV)
+                scale = torch.zeros(btotal, device=DEV)
+                for a, k, b, nb in zip(starts, n, bstarts, blocks):
+                    pad = torch.nn.functional.pad(x[a:a + k], (0, nb * BLOCK - k)).view(nb, BLOCK)
+                    top = pad.abs().amax(1)
+                    scale[b:b + nb] = top / E4M3_MAX
+                    code[a:a + k] = (pad / (top / E4M3_MAX)[:, None]).clamp(-E4M3_MAX, E4M3_MAX).to(code.dtype).view(-1)[:k]
+                flat[name], flat[name + "_scale"] = code, scale
+            s["m_scales"], s["v_scales"] = views(flat["m_scale"], bstarts, blocks), views(flat["v_scale"], bstarts, blocks)
+        for name in ("g", "master", "m", "v", "w"):
+            s[name] = views(flat[name], starts, n)
+        s["decay"] = [0.1 if yes else 0.0 for _, yes in sizes]
+        s["step"], s["lr"], s["seed"] = 1000, 1e-4, seed & 0x7FFFFFFF
+    return s
+
+
+# -------------------------------------------------------------------------------------- plain forms
+
+def _plain_rotary(s):
+    c, x, y = s["case"], s["x"], s["y"]
+    T, h, d, rot = c["T"], c["heads"], c["d"], c["rot"]
+    pos = s["pos"] if s["pos"] is not None else torch.arange(T, device=DEV) % c["seq"]
+    turn = pos.double()[:, None] * s["freq"][None]
+    cos, sin = (t.float()[:, None] * s["amplitude"] for t in (torch.cos(turn), torch.sin(turn)))
+    if c["inverse"]:
+        sin = -sin
+    v = x[:, :h * d].unflatten(1, (h, d))
+    part = v[..., :rot].float()
+    if c["layout"] == "halves":
+        a, b = part[..., :rot // 2], part[..., rot // 2:]
+        new = torch.cat([a * cos - b * sin, b * cos + a * sin], -1)
+    else:
+        a, b = part[..., 0::2], part[..., 1::2]
+        new = torch.stack([a * cos - b * sin, b * cos + a * sin], -1).flatten(-2)
+    out = y.unflatten(1, (h, d))
+    out[..., :rot] = new.to(y.dtype)
+    if not c["in_place"]:
+        out[..., rot:] = v[..., rot:]
+        return y
+    return x
+
+
+def _plain_cross(s):
+    c = s["case"]
+    b, sq, sk, h, hk, d = (c[n] for n in ("batch", "sq", "sk", "heads", "kv_heads", "d"))
+    gr, act, scale = h // hk, s["q"].dtype, d ** -0.5
+    q = s["q"].float().view(b, sq, hk, gr, d).permute(0, 2, 3, 1, 4).reshape(b, hk, gr * sq, d)
+    k, v = (t.reshape(b, sk, hk, d).transpose(1, 2).contiguous() for t in s["kv"].float().split(hk * d, 1))
+    z = torch.matmul(q, k.transpose(2, 3).contiguous()) * scale
+    if s["len"] is not None:
+        z = z.masked_fill(torch.arange(sk, device=DEV)[None, None, None] >= s["len"][:, None, None, None], -math.inf)
+    top = z.amax(3, keepdim=True)
+    top = torch.where(top == -math.inf, torch.zeros_like(top), top)
+    e = torch.exp(z - top)
+    total = e.sum(3, keepdim=True)
+    lse = (top + torch.log(total))[..., 0]
+    p = e / torch.where(total == 0, torch.ones_like(total), total)
+
+    def back(t):                      # [b, hk, gr * sq, d] -> rows of the queries
+        return t.view(b, hk, gr, sq, d).permute(0, 3, 1, 2, 4).reshape(b * sq, h * d)
+    ctx = torch.matmul(p, v)
+    out = {"ctx": back(ctx).to(act), "lse": lse.view(b, hk, gr, sq).reshape(b, h, sq)}
+    if c["step"]:
+        g = s["dctx"].float().view(b, sq, hk, gr, d).permute(0, 2, 3, 1, 4).reshape(b, hk, gr * sq, d)
+        dv = torch.matmul(p.transpose(2, 3).contiguous(), g)
+        ds = p * (torch.matmul(g, v.transpose(2, 3).contiguous()) - (g * ctx).sum(3, keepdim=True)) * scale
+        out["dq"] = back(torch.matmul(ds, k)).to(act)
+        dk = torch.matmul(ds.transpose(2, 3).contiguous(), q)
+        out["dkv"] = torch.cat([t.transpose(1, 2).reshape(b * sk, hk * d) for t in (dk, dv)], 1).to(act)
+    return out
+
+
+CLIP_LOW, CLIP_HIGH, KL, BETA = 0.2, 0.28, 0.05, 0.1
+
+
+def _plain_policy(s):
+    c = s["case"]
+    z, y = s["logits"].float(), s["labels"].long()[:, None]
+    counts = torch.ones_like(s["old"], dtype=torch.bool) if s["mask"] is None else s["mask"] != 0
+    top = z.amax(1, keepdim=True)
+    z = z - top
+    e = torch.exp(z)
+    total = e.sum(1, keepdim=True)
+    p, log_total = e / total, torch.log(total)
+    logp = (z.gather(1, y) - log_total)[:, 0]
+    entropy = log_total[:, 0] - (p * z).sum(1)
+    ratio = torch.exp(logp - s["old"])
+    free, held = ratio * s["adv"], ratio.clamp(1 - CLIP_LOW, 1 + CLIP_HIGH) * s["adv"]
+    loss = -torch.minimum(free, held) - c["ent"] * entropy
+    coef = torch.where(free <= held, -free, torch.zeros_like(free))
+    kl = torch.zeros_like(loss)
+    if s["ref"] is not None:
+        away = s["ref"] - logp
+        kl = torch.expm1(away) - away
+        loss = loss + KL * kl
+        coef = coef - KL * torch.expm1(away)
+    d = p * (c["ent"] * (z - log_total + entropy[:, None]) - coef[:, None])
+    d.scatter_add_(1, y, coef[:, None])
+    none = torch.zeros_like(loss)
+    return {"logp": torch.where(counts, logp, none), "loss": torch.where(counts, loss, none),
+            "kl": torch.where(counts, kl, none), "entropy": torch.where(counts, entropy, none),
+            "dlogits": torch.where(counts[:, None], d * s["scale"], 0.0).to(s["dlogits"].dtype)}
+
+
+def _plain_preference(s):
+    c = s["case"]
+    n, S = 2 * c["pairs"], c["seq"]
+    z, y, counts = s["logits"].float(), s["labels"].long()[:, None], s["mask"] != 0
+    z = z - z.amax(1, keepdim=True)
+    e = torch.exp(z)
+    total = e.sum(1, keepdim=True)
+    logp = (z.gather(1, y) - torch.log(total))[:, 0]
+    seqs = torch.where(counts, logp, 0.0).view(n, S).double().sum(1)
+    chosen, rejected = (seqs - s["ref"].double()).view(2, c["pairs"])
+    margin = BETA * (chosen - rejected)
+    sg = torch.nn.functional.logsigmoid
+    loss = -(1 - c["smoothing"]) * sg(margin) - c["smoothing"] * sg(-margin)
+    coef = (torch.sigmoid(margin) - (1 - c["smoothing"])) * BETA / c["pairs"]
+    coef = torch.cat([coef, -coef]).float().repeat_interleave(S)
+    coef = torch.where(counts, coef, 0.0)[:, None]
+    d = -coef * (e / total)
+    d.scatter_add_(1, y, coef)
+    return {"logp_seq": seqs.float(), "loss": loss.float(), "dlogits": d.to(s["dlogits"].dtype)}
+
+
+def _mix(x):
+    """32 well-mixed bits of 32 bits (a number or a tensor of 64-bit integers)."""
+    x = x ^ (x >> 16)
+    x = (x * 0x7FEB352D) & M32
+    x = x ^ (x >> 15)
+    x = (x * 0x846CA68B) & M32
+    return x ^ (x >> 16)
+
+
+def _key(seed, step, k):
+    return _mix((_mix((seed + step * 0x9E3779B9) & M32) + k * 0x85EBCA6B) & M32)
+
+
+def _to_codes(x, top, up, least):
+    """x >= 0 in units of its block's largest / 448, rounded to 3 bits behind the leading one: down or up, as `up` in [0, 1) says."""
+    q = (x * (E4M3_MAX / torch.where(top > 0, top, torch.ones_like(top)))).clamp(max=E4M3_MAX)
+    step = torch.exp2((torch.frexp(q)[1] - 1).clamp(min=-6).to(q.dtype) - 3)
+    q = (torch.floor(q / step + up) * step).clamp(max=E4M3_MAX)
+    return torch.where(x > 0, q.clamp(min=2.0 ** -9), q) if least else q
+
+
+def _plain_adamw_one(k, s, c1, c2, key):
+    g, master, w = s["g"][k], s["master"][k], s["w"][k]
+    b1, b2, eps, lr, n = 0.9, 0.999, 1e-8, s["lr"], g.numel()
+    eight = s["case"]["bits"] == 8
+    if eight:
+        nb = -(-n // BLOCK)
+        ms, vs = (s[t][k].repeat_interleave(BLOCK)[:n] for t in ("m_scales", "v_scales"))
+        m, v = s["m"][k].float() * ms, (s["v"][k].float() * vs).square()
+    else:
+        m, v = s["m"][k], s["v"][k]
+    m = b1 * m + (1 - b1) * g
+    v = b2 * v + (1 - b2) * g * g
+    master.copy_(master * (1 - lr * s["decay"][k]) - lr * (m * c1) / (torch.sqrt(v * c2) + eps))
+    w.copy_(master)
+    if not eight:
+        s["m"][k].copy_(m)
+        s["v"][k].copy_(v)
+        return
+    bits = _mix((torch.arange(n, device=DEV) & M32) ^ key)
+    for name, x, b, least in (("m", m, bits & 0xFFFF, False), ("v", torch.sqrt(v), bits >> 16, True)):
+        top = torch.nn.functional.pad(x.abs(), (0, nb * BLOCK - n)).view(nb, BLOCK).amax(1)
+        s[name + "_scales"][k].copy_(top / E4M3_MAX)
+        q = _to_codes(x.abs(), top.repeat_interleave(BLOCK)[:n], (b.float() + 0.5) / 65536, least)
+        s[name][k].copy_((torch.sign(x) * q).to(torch.float8_e4m3fn))
+
+
+def _plain_adamw(s):
+    s["step"] += 1
+    c1, c2 = 1 / (1 - 0.9 ** s["step"]), 1 / (1 - 0.999 ** s["step"])
+    list(map(lambda k: _plain_adamw_one(k, s, c1, c2, _key(s["seed"], s["step"], k)), range(len(s["g"]))))
+    return {k: t for k, t in s["flat"].items() if k != "g"}
+
+
+# -------------------------------------------------------------------------------- framework's calls
+
+def _own_rotary(s):
+    B, c = _lib(), s["case"]
+    B.bk_rotary(s["x"], s["freq"], s["y"], c["heads"], c["d"], pos=s["pos"], seq=c["seq"],
+                interleaved=c["layout"] == "neighbours", inverse=c["inverse"], amplitude=s["amplitude"])
+    return s["x"] if c["in_place"] else s["y"]
+
+
+def _own_cross(s):
+    B, c = _lib(), s["case"]
+    Hkv = c["kv_heads"] * c["d"]
+    k, v = s["kv"][:, :Hkv], s["kv"][:, Hkv:]
+    B.bk_cross_attention_fwd(s["q"], k, v, s["ctx"], s["lse"], c["batch"], c["heads"], c["kv_heads"], kv_len=s["len"])
+    out = {"ctx": s["ctx"], "lse": s["lse"]}
+    if c["step"]:
+        B.bk_cross_attention_bwd(s["q"], k, v, s["ctx"], s["lse"], s["dctx"], s["dq"], s["dkv"][:, :Hkv], s["dkv"][:, Hkv:],
+                                 c["batch"], c["heads"], c["kv_heads"], kv_len=s["len"])
+        out["dq"], out["dkv"] = s["dq"], s["dkv"]
+    return out
+
+
+def _own_policy(s):
+    _lib().bk_policy_loss(s["logits"], s["labels"], s["old"], s["adv"], s["logp"], s["loss"], s["dlogits"], mask=s["mask"],
+                          ref_logp=s["ref"], kl_tok=s["kl"], entropy=s["ent"], clip_low=CLIP_LOW, clip_high=CLIP_HIGH,
+                          kl_coef=KL, ent_coef=s["case"]["ent"], scale=s["scale"])
+    return {"logp": s["logp"], "loss": s["loss"], "kl": s["kl"], "entropy": s["ent"], "dlogits": s["dlogits"]}
+
+
+def _own_preference(s):
+    B, c = _lib(), s["case"]
+    B.bk_preference_loss_fwd(s["logits"], s["labels"], s["ref"], s["lse"], s["logp"], s["logp_seq"], s["loss"], c["pairs"],
+                             BETA, c["smoothing"], mask=s["mask"])
+    B.bk_preference_loss_bwd(s["logits"], s["labels"], s["ref"], s["lse"], s["logp_seq"], s["dlogits"], c["pairs"], BETA,
+                             c["smoothing"], scale=1.0 / c["pairs"], mask=s["mask"])
+    return {"logp_seq": s["logp_seq"], "loss": s["loss"], "dlogits": s["dlogits"]}
+
+
+def _own_adamw(s):
+    s["step"] += 1
+    _lib().bk_adamw_group(s["g"], s["master"], s["m"], s["v"], s["w"], s["step"], lr=s["lr"], decay=s["decay"],
+                          m_scales=s.get("m_scales"), v_scales=s.get("v_scales"), seed=s["seed"])
+    return {k: t for k, t in s["flat"].items() if k != "g"}
+
+
+def run(state):
+    op = state["case"]["op"]
+    if own:
+        return {"rotary": _own_rotary, "cross": _own_cross, "policy": _own_policy, "preference": _own_preference,
+                "adamw": _own_adamw}[op](state)
+    return {"rotary": _plain_rotary, "cross": _plain_cross, "policy": _plain_policy, "preference": _plain_preference,
+            "adamw": _plain_adamw}[op](state)
+
+
+# ------------------------------------------------------------------------------- definition, 64 bits
+
+def _exact_rotary(s):
+    c = s["case"]
+    h, d, rot, n = c["heads"], c["d"], c["rot"], c["rot"] // 2
+    base = c["base"]
+    if c["scaling"] == "stretched" and rot > 2:
+        base = math.exp(math.log(base) + math.log(c["factor"]) * rot / (rot - 2))
+    freq, amp = [], 1.0
+    for i in range(n):
+        f = math.exp(-2 * i / rot * math.log(base))
+        if c["scaling"] == "linear":
+            f /= c["factor"]
+        elif c["scaling"] == "parts":
+            keep = min(1.0, max(0.0, (4096 * f / (2 * math.pi) - 1) / 31))
+            f = keep * f + (1 - keep) * f / c["factor"]
+            amp = 1 + 0.1 * math.log(c["factor"])
+        freq.append(f)
+    pos = torch.arange(c["T"], device=DEV) % c["seq"] if s["pos"] is None else s["pos"]
+    # each pair as a complex number, turned by multiplying with e^(i angle)
+    angle = pos.double()[:, None] * torch.tensor(freq, dtype=torch.float64, device=DEV)[None]
+    turn = torch.polar(torch.full_like(angle, amp), -angle if c["inverse"] else angle)
+    out = s["x"].double() if c["in_place"] else s["x"][:, :h * d].double()
+    first = [(i, i + n) if c["layout"] == "halves" else (2 * i, 2 * i + 1) for i in range(n)]
+    a, b = (torch.tensor([p[j] for p in first], device=DEV) for j in (0, 1))
+    for k in range(h):
+        head = out[:, k * d:(k + 1) * d]
+        z = torch.complex(head[:, a], head[:, b]) * turn
+        head[:, a], head[:, b] = z.real, z.imag
+    return out
+
+
+def _exact_cross(s):
+    c = s["case"]
+    b, sq, sk, h, hk, d = (c[n] for n in ("batch", "sq", "sk", "heads", "kv_heads", "d"))
+    q = s["q"].double()
+    ctx, lse = torch.zeros_like(q), torch.full((b, h, sq), -math.inf, dtype=torch.float64, device=DEV)
+    dq, dkv = torch.zeros_like(q), torch.zeros(b * sk, 2 * hk * d, dtype=torch.float64, device=DEV)
+    lens = [sk] * b if s["len"] is None else s["len"].tolist()
+    for i in range(b):
+        if lens[i] == 0:
+            continue
+        rows, keys = slice(i * sq, (i + 1) * sq), slice(i * sk, i * sk + lens[i])
+        for j in range(h):
+            cols = slice(j * d, (j + 1) * d)
+            at = [slice(o + (j // (h // hk)) * d, o + (j // (h // hk) + 1) * d) for o in (0, hk * d)]
+            leaves = [t.clone().requires_grad_(c["step"]) for t in
+                      (q[rows, cols], s["kv"][keys, at[0]].double(), s["kv"][keys, at[1]].double())]
+            with torch.enable_grad():
+                z = leaves[0] @ leaves[1].T / math.sqrt(d)
+                o = torch.softmax(z, 1) @ leaves[2]
+            ctx[rows, cols], lse[i, j] = o.detach(), torch.logsumexp(z.detach(), 1)
+            if c["step"]:
+                grads = torch.autograd.grad(o, leaves, s["dctx"][rows, cols].double())
+                dq[rows, cols] = grads[0]
+                for k in (0, 1):
+                    dkv[keys, at[k]] += grads[1 + k]
+    out = {"ctx": ctx, "lse": lse}
+    return dict(out, dq=dq, dkv=dkv) if c["step"] else out
+
+
+def _exact_policy(s):
+    c, parts = s["case"], []
+    for t0 in range(0, c["T"], 512):
+        cut = slice(t0, min(t0 + 512, c["T"]))
+        z = s["logits"][cut].double().requires_grad_(True)
+        with torch.enable_grad():
+            lp = torch.log_softmax(z, 1)
+            logp = lp.gather(1, s["labels"][cut].long()[:, None])[:, 0]
+            entropy = -(lp.exp() * lp).sum(1)
+            r, A = torch.exp(logp - s["old"][cut].double()), s["adv"][cut].double()
+            loss = -torch.minimum(r * A, r.clamp(1 - CLIP_LOW, 1 + CLIP_HIGH) * A) - c["ent"] * entropy
+            kl = torch.zeros_like(loss)
+            if s["ref"] is not None:
+                kl = torch.exp(s["ref"][cut].double() - logp) - (s["ref"][cut].double() - logp) - 1
+                loss = loss + KL * kl
+            counts = torch.ones_like(loss) if s["mask"] is None else (s["mask"][cut] != 0).double()
+            total = (loss * counts).sum() * s["scale"]
+        d, = torch.autograd.grad(total, z)
+        parts.append([t.detach() for t in (logp * counts, loss * counts, kl * counts, entropy * counts, d)])
+    return dict(zip(("logp", "loss", "kl", "entropy", "dlogits"), (torch.cat(p) for p in zip(*parts))))
+
+
+def _exact_preference(s):
+    c = s["case"]
+    n, S, eps = 2 * c["pairs"], c["seq"], c["smoothing"]
+    seqs = torch.zeros(n, dtype=torch.float64, device=DEV)
+    for i in range(n):
+        lp = torch.log_softmax(s["logits"][i * S:(i + 1) * S].double(), 1)
+        picked = lp.gather(1, s["labels"][i * S:(i + 1) * S].long()[:, None])[:, 0]
+        seqs[i] = picked[s["mask"][i * S:(i + 1) * S] != 0].sum()
+    total = seqs.clone().requires_grad_(True)
+    with torch.enable_grad():
+        ratio = total - s["ref"].double()
+        margin = BETA * (ratio[:c["pairs"]] - ratio[c["pairs"]:])
+        p = 1 / (1 + torch.exp(-margin))
+        loss = -(1 - eps) * torch.log(p) - eps * torch.log1p(-p)
+        mean = loss.mean()
+    coef, = torch.autograd.grad(mean, total)
+    d = torch.zeros(n * S, c["V"], dtype=torch.float64, device=DEV)
+    for i in range(n):
+        rows = torch.nonzero(s["mask"][i * S:(i + 1) * S])[:, 0] + i * S
+        p = torch.softmax(s["logits"][rows].double(), 1)
+        p[torch.arange(len(rows), device=DEV), s["labels"][rows].long()] -= 1
+        d[rows] = -coef[i] * p
+    return {"logp_seq": seqs, "loss": loss.detach(), "dlogits": d}
+
+
+def _exact_adamw(s):
+    """The codes of moments in 8 bits have no value of their own: either neighbour is a right one."""
+    t = s["step"] + 1
+    out = {k: None for k in s["flat"] if k != "g"}
+    out["master"] = s["flat"]["master"].double()
+    # rounded from the master weights: the neighbour of a tie has its own value, which is no error of the step
+    out["w"] = s["flat"]["w"].double()
+    if s["case"]["bits"] == 32:
+        out["m"], out["v"] = s["flat"]["m"].double(), s["flat"]["v"].double()
+    scales = {"m_scale": [], "v_scale": []}
+    for k, g in enumerate(s["g"]):
+        a = g.storage_offset()
+        cut, g = slice(a, a + g.numel()), g.double()
+        m, v = s["m"][k].double(), s["v"][k].double()
+        if s["case"]["bits"] == 8:
+            block = torch.arange(len(g), device=DEV) // BLOCK
+            m, v = m * s["m_scales"][k].double()[block], (v * s["v_scales"][k].double()[block]) ** 2
+        m, v = m + (g - m) * (1 - 0.9), v + (g * g - v) * (1 - 0.999)
+        step = (m / (1 - 0.9 ** t)) / (torch.sqrt(v / (1 - 0.999 ** t)) + 1e-8) + s["decay"][k] * s["master"][k].double()
+        out["master"][cut] -= s["lr"] * step
+        out["w"][cut] = out["master"][cut]
+        if s["case"]["bits"] == 32:
+            out["m"][cut], out["v"][cut] = m, v
+        else:
+            for name, x in (("m_scale", m.abs()), ("v_scale", v.sqrt())):
+                tops = torch.zeros(len(s[name + "s"][k]), dtype=torch.float64, device=DEV)
+                scales[name].append(tops.scatter_reduce_(0, block, x, "amax") / E4M3_MAX)
+    out.update({name: torch.cat(parts) for name, parts in scales.items() if parts})
+    return out
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    with torch.no_grad():
+        return {"rotary": _exact_rotary, "cross": _exact_cross, "policy": _exact_policy, "preference": _exact_preference,
+                "adamw": _exact_adamw}[case["op"]](s)
+
+
+# ----------------------------------------------------------------------------------- necessary work
+
+def work(case):
+    e, op = 2 if case["dtype"] == "bf16" else 4, case["op"]
+    if op == "rotary":
+        part = case["rot"] if case["in_place"] else case["d"]
+        n = case["T"] * case["heads"]
+        return {"bytes": 2 * n * part * e + 4 * case["rot"] + (4 * case["T"] if case["far"] else 0), "flops": 3 * n * case["rot"]}
+    if op == "cross":
+        b, sq, sk, h, hk, d = (case[n] for n in ("batch", "sq", "sk", "heads", "kv_heads", "d"))
+        share = 1.0 if case["lengths"] == "full" else (1 + (b - 1) / 2) / b     # of the keys that count, on average
+        rows, keys, pairs = b * sq * h * d, int(2 * b * sk * hk * d * share), int(b * h * sq * sk * d * share)
+        if not case["step"]:
+            return {"bytes": (2 * rows + keys) * e + 4 * b * sq * h, "flops": 4 * pairs}
+        return {"bytes": (4 * rows + keys + 2 * b * sk * hk * d) * e + 4 * b * sq * h, "flops": 14 * pairs}
+    if op == "policy":
+        T, V = case["T"], case["V"]
+        return {"bytes": int(T * V * e * (1 + case["counted"])) + 32 * T, "flops": int(8 * T * V * case["counted"])}
+    if op == "preference":
+        T, V = 2 * case["pairs"] * case["seq"], case["V"]
+        return {"bytes": int(T * V * e * 1.5) + 12 * T, "flops": 3 * T * V}   # about half of the tokens count
+    n = sum(k for k, _ in _sizes(case))
+    state = 16 if case["bits"] == 32 else 4 + 16 / BLOCK
+    return {"bytes": int(n * (12 + e + state)), "flops": 14 * n}
