@@ -238,7 +238,7 @@ def prepare(case, seed):
             t = torch.arange(S, device=DEV)[None]
             s["mask"] = ((t >= first) & (t < last)).to(torch.uint8).reshape(-1)
             s["ref"] = ((now + 0.3 * normal(T)) * s["mask"]).view(n, S).double().sum(1).float()
-            s["lse"], s["logp_seq"], s["loss"] = (torch.empty(k, device=DEV) for k in (T, n, case["pairs"]))
+            s["lse"], s["logp_seq"], s["margin"], s["loss"] = (torch.empty(k, device=DEV) for k in (T, n, n // 2, n // 2))
     else:
         sizes = _sizes(case)
         n = [k for k, _ in sizes]
@@ -378,7 +378,7 @@ def _plain_preference(s):
     coef = torch.where(counts, coef, 0.0)[:, None]
     d = -coef * (e / total)
     d.scatter_add_(1, y, coef)
-    return {"logp_seq": seqs.float(), "loss": loss.float(), "dlogits": d.to(s["dlogits"].dtype)}
+    return {"logp_seq": seqs.float(), "margin": margin.float(), "loss": loss.float(), "dlogits": d.to(s["dlogits"].dtype)}
 
 
 def _mix(x):
@@ -466,11 +466,11 @@ def _own_policy(s):
 
 def _own_preference(s):
     B, c = _lib(), s["case"]
-    B.bk_preference_loss_fwd(s["logits"], s["labels"], s["ref"], s["lse"], s["logp"], s["logp_seq"], s["loss"], c["pairs"],
-                             BETA, c["smoothing"], mask=s["mask"])
-    B.bk_preference_loss_bwd(s["logits"], s["labels"], s["ref"], s["lse"], s["logp_seq"], s["dlogits"], c["pairs"], BETA,
-                             c["smoothing"], scale=1.0 / c["pairs"], mask=s["mask"])
-    return {"logp_seq": s["logp_seq"], "loss": s["loss"], "dlogits": s["dlogits"]}
+    B.bk_preference_loss_fwd(s["logits"], s["labels"], s["ref"], s["lse"], s["logp"], s["logp_seq"], s["margin"], s["loss"],
+                             BETA, smoothing=c["smoothing"], mask=s["mask"])
+    B.bk_preference_loss_bwd(s["logits"], s["labels"], s["lse"], s["margin"], s["dlogits"], BETA, smoothing=c["smoothing"],
+                             scale=1.0 / c["pairs"], mask=s["mask"])
+    return {"logp_seq": s["logp_seq"], "margin": s["margin"], "loss": s["loss"], "dlogits": s["dlogits"]}
 
 
 def _own_adamw(s):
@@ -594,7 +594,7 @@ def _exact_preference(s):
         p = torch.softmax(s["logits"][rows].double(), 1)
         p[torch.arange(len(rows), device=DEV), s["labels"][rows].long()] -= 1
         d[rows] = -coef[i] * p
-    return {"logp_seq": seqs, "loss": loss.detach(), "dlogits": d}
+    return {"logp_seq": seqs, "margin": margin.detach(), "loss": loss.detach(), "dlogits": d}
 
 
 def _exact_adamw(s):
