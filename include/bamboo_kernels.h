@@ -123,6 +123,93 @@ int bk_softmax_xent_bwd(int dtype, int T, int V, const void* logits, const int32
 /* out[0] = scale * (in[0] + ... + in[n-1]) in a fixed order (the mean loss of a micro-batch). */
 int bk_ordered_sum(int64_t n, const float* in, float scale, float* out, void* stream);
 
+/* ---- operators of a training step around the stage: what a model that reads an encoder, or is trained further from
+ * preferences or rewards, puts between the calls above.  Here a row of a matrix may be followed by other columns: ld* is
+ * the distance between rows in elements.  Outputs must not overlap inputs except where it says so.  Calls work on the
+ * current device, which the stream and all pointers belong to; nothing is kept from one call for the next.
+ *
+ * Rotary positions, between the QKV product and the attention: in each of `heads` heads of row t (columns h*d .. h*d+d-1),
+ * pair i of the first rot features is turned by the angle pos[t] * freq[i]:
+ *   (a, b) -> amplitude * (a cos - b sin, b cos + a sin),
+ * the pair being features (i, i + rot/2), or (2i, 2i + 1) if interleaved != 0.  inverse != 0 turns the other way: the
+ * backward, from the gradient at y to that at x.  Features rot .. d-1 are passed on.  y may be x (with ldy = ldx); for
+ * queries and keys of a packed qkv[T,3H] in place: heads = 2 * heads, ldx = 3H.
+ * pos: device int32 [T], any sign, or NULL for t mod seq.  freq: device double [rot/2] (bk_rotary_frequencies).  Angles
+ * are formed in 64 bits.  2 <= rot <= d <= 512, rot even. */
+int bk_rotary(int dtype, int T, int seq, int heads, int d, int rot, int interleaved, int inverse, const void* x,
+              int64_t ldx, const int32_t* pos, const double* freq, float amplitude, void* y, int64_t ldy, void* stream);
+/* freq (HOST double [rot/2]) = base^(-2i/rot), for a context stretched by `factor` >= 1:
+ * scaling 0  as it is;  1  all divided by factor;  2  base * factor^(rot/(rot-2)) in the place of base (the slowest pair is
+ * divided by factor, the fastest stays);  3  by parts: a pair that makes r turns in `length` positions is kept to
+ * w = clamp((r - 1) / 31, 0, 1) and divided by factor to 1 - w, and *amplitude = 0.1 ln(factor) + 1 instead of 1.
+ * length: the context the model was trained on (scaling 3 only).  amplitude may be NULL.  Runs on the host. */
+int bk_rotary_frequencies(int rot, double base, int scaling, double factor, int length, double* freq, float* amplitude);
+
+/* Softmax attention of queries over the states of an encoder, of another length.  Queries q[batch*sq, heads*d] (row
+ * stride ldq), keys and values k, v[batch*sk, kv_heads*d] (row stride ldkv; halves of one packed projection, or two
+ * matrices); query head h reads key head h / (heads / kv_heads); scores scaled by 1/sqrt(d); 1 <= d <= 128.
+ * kv_len: device int32 [batch], keys that count of each sample (the first ones; clamped to 0 .. sk), or NULL for all; keys
+ * and values behind them are never read.  ctx[batch*sq, heads*d] (row stride ldc), lse[batch,heads,sq] fp32.  A sample
+ * without keys has ctx = 0 and lse = -inf.
+ * scratch: fp32, bk_cross_attention_scratch_floats(..) floats, 16-byte aligned, used by this call alone.
+ * impl: 0 automatic, 1 fp32 arithmetic on the matrix cores (any d and alignment), 2 bf16 (BAMBOO_E_STATE if it does not
+ * cover the shape: bf16, d 64 or 128, strides multiples of 8, pointers 16-byte aligned). */
+int bk_cross_attention_fwd(int dtype, int impl, int batch, int sq, int sk, int heads, int kv_heads, int d, const void* q,
+                           int64_t ldq, const void* k, const void* v, int64_t ldkv, const int32_t* kv_len, void* ctx,
+                           int64_t ldc, float* lse, float* scratch, void* stream);
+/* dq, dk, dv (strides lddq, lddkv) from dctx (stride lddc), recomputing the probabilities from lse.  Keys that do not count
+ * get zeros; the gradients of a key head are summed over the query heads that read it.  Fixed order, no atomics. */
+int bk_cross_attention_bwd(int dtype, int impl, int batch, int sq, int sk, int heads, int kv_heads, int d, const void* q,
+                           int64_t ldq, const void* k, const void* v, int64_t ldkv, const int32_t* kv_len,
+                           const void* ctx, int64_t ldc, const float* lse, const void* dctx, int64_t lddc, void* dq,
+                           int64_t lddq, void* dk, void* dv, int64_t lddkv, float* scratch, void* stream);
+uint64_t bk_cross_attention_scratch_floats(int batch, int sq, int sk, int heads, int kv_heads, int d);
+
+/* Clipped policy loss with a KL and an entropy term, and its gradient in the same pass.  Per token t, with
+ * logp = log softmax(logits[t,:])[labels[t]], r = exp(logp - old_logp[t]), u = ref_logp[t] - logp:
+ *   loss_tok[t] = -min(r adv[t], clip(r, 1 - clip_low, 1 + clip_high) adv[t]) + kl_coef (exp(u) - u - 1) - ent_coef H
+ *   dlogits[t,:] = scale * d loss_tok[t] / d logits[t,:]       (where both sides of the min are equal: the unclipped one's)
+ * H: entropy of the token's distribution.  mask: device bytes [T], 0 = the token does not count (its logits are not read;
+ * all it gets is zeros), or NULL.  ref_logp NULL: no KL term.  Any V, strides ldl, ldd in elements; labels outside [0, V) are
+ * clamped.  Outputs [T] fp32: logp, loss_tok, and, unless NULL, kl_tok (the term without its coefficient) and entropy;
+ * dlogits NULL: no gradient; dlogits may be logits (with ldd = ldl).  logits of -inf take no part; a NaN, +inf or a row
+ * of -inf alone makes the row NaN.  The mean over the tokens: bk_ordered_sum. */
+int bk_policy_loss(int dtype, int T, int V, const void* logits, int64_t ldl, const int32_t* labels, const uint8_t* mask,
+                   const float* old_logp, const float* ref_logp, const float* adv, float clip_low, float clip_high,
+                   float kl_coef, float ent_coef, float scale, float* logp, float* loss_tok, float* kl_tok,
+                   float* entropy, void* dlogits, int64_t ldd, void* stream);
+
+/* Preference loss over pairs of sequences.  logits[2*pairs*seq, V]: the chosen sequences, then the rejected ones in the
+ * same order.  logp_seq[2*pairs] = sums of the counting tokens' log-probabilities, and per pair
+ *   margin = beta ((logp_chosen - ref_chosen) - (logp_rejected - ref_rejected))
+ *   loss = -(1 - smoothing) log sigmoid(margin) - smoothing log sigmoid(-margin)
+ * ref_logp[2*pairs]: the reference model's sums.  mask, labels, V, ldl: as above.  lse[T], logp[T] (0 for tokens that do not
+ * count), T = 2*pairs*seq, margin[pairs], loss[pairs]: fp32 outputs; sums over a sequence are taken in 64 bits, of terms in
+ * 64 bits: scratch, T doubles, used by this call alone. */
+int bk_preference_loss_fwd(int dtype, int pairs, int seq, int V, const void* logits, int64_t ldl, const int32_t* labels,
+                           const uint8_t* mask, const float* ref_logp, float beta, float smoothing, float* lse,
+                           float* logp, float* logp_seq, float* margin, float* loss, double* scratch, void* stream);
+/* dlogits[t,:] = scale * d loss[pair of t] / d logits[t,:]; dlogits may be logits (with ldd = ldl). */
+int bk_preference_loss_bwd(int dtype, int pairs, int seq, int V, const void* logits, int64_t ldl, const int32_t* labels,
+                           const uint8_t* mask, const float* lse, const float* margin, float beta, float smoothing,
+                           float scale, void* dlogits, int64_t ldd, void* stream);
+
+/* One AdamW step over n tensors, step >= 1.  Host arrays of n: numel (0 is allowed), device pointers g (fp32 gradients),
+ * master (fp32 weights), m, v, w (storage dtype, = the new master weights rounded), decay (the tensor's weight decay):
+ *   m <- beta1 m + (1-beta1) g,  v <- beta2 v + (1-beta2) g^2,
+ *   master <- master (1 - lr decay) - lr (m / (1-beta1^step)) / (sqrt(v / (1-beta2^step)) + eps)
+ * moment_bits 32: m, v fp32; m_scale, v_scale NULL.  8: m, v codes of one byte (e4m3) and m_scale, v_scale fp32
+ * [ceil(numel/256)]: element i of m is code * m_scale[i/256], the ROOT of element i of v is code * v_scale[i/256]; all
+ * zero bits are zero moments.  The step uses the moments before they are rounded to codes; the rounding goes up or down by
+ * bits that depend on (seed, step, the tensor's place in the list, the element) alone, so that replicas that make the
+ * same calls stay equal to the bit.  A gradient that is not finite makes its element's moments, an infinite one its whole
+ * block's, NaN.  No two tensors may overlap.  Any alignment of an element; the fast form takes pointers aligned to 16
+ * bytes (w and codes: to four elements). */
+int bk_adamw_group(int dtype, int moment_bits, int n, const int64_t* numel, const float* const* g, float* const* master,
+                   void* const* m, void* const* v, float* const* m_scale, float* const* v_scale, void* const* w,
+                   const double* decay, double lr, double beta1, double beta2, double eps, int step, uint32_t seed,
+                   void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -15,6 +15,9 @@ Modules
   ends      the two ends of the model that the wrap-around stage works on (Section 5.1: the
             last node fetches the input samples to run the first node's layers): token and
             position embedding at the front, LM head and mean cross-entropy at the back
+  operators rotary positions, attention over an encoder's states, policy and preference
+            losses, AdamW over many tensors (not part of the paper's method: what a user
+            of the stage's kernels trains with them)
   optim     Adam update (Section 7 names the optimizer) and replica weight
             synchronisation (Section 5.1 requires equal parameters)
 

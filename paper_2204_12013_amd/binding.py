@@ -137,6 +137,16 @@ _SIGS = {
     "bk_gemm_tile": (C.c_int, [C.c_int]),
     "bk_gemm_stages": (C.c_int, [C.c_int]),
     "bk_adam": (C.c_int, [C.c_int, C.c_int64] + [_vp] * 5 + [C.c_float] * 4 + [C.c_int, _vp]),
+    "bk_rotary": (C.c_int, [C.c_int] * 8 + [_vp, _i64, _vp, _vp, _f32, _vp, _i64, _vp]),
+    "bk_rotary_frequencies": (C.c_int, [C.c_int, C.c_double, C.c_int, C.c_double, C.c_int, _vp, C.POINTER(_f32)]),
+    "bk_cross_attention_fwd": (C.c_int, [C.c_int] * 8 + [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _vp]),
+    "bk_cross_attention_bwd": (C.c_int, [C.c_int] * 8 + [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _vp, _i64,
+                                                         _vp, _vp, _i64, _vp, _vp]),
+    "bk_cross_attention_scratch_floats": (C.c_uint64, [C.c_int] * 6),
+    "bk_policy_loss": (C.c_int, [C.c_int] * 3 + [_vp, _i64] + [_vp] * 5 + [_f32] * 5 + [_vp] * 5 + [_i64, _vp]),
+    "bk_preference_loss_fwd": (C.c_int, [C.c_int] * 4 + [_vp, _i64] + [_vp] * 3 + [_f32] * 2 + [_vp] * 7),
+    "bk_preference_loss_bwd": (C.c_int, [C.c_int] * 4 + [_vp, _i64] + [_vp] * 4 + [_f32] * 3 + [_vp, _i64, _vp]),
+    "bk_adamw_group": (C.c_int, [C.c_int] * 3 + [_vp] * 9 + [C.c_double] * 4 + [C.c_int, C.c_uint32, _vp]),
 }
 EXPORTS = tuple(_SIGS)
 for _name, (_res, _args) in _SIGS.items():
@@ -592,6 +602,204 @@ def bk_softmax_xent_bwd(logits, labels, lse, scale, dlogits, stream=None):
 
 def bk_ordered_sum(x, scale, out, stream=None):
     _check(lib.bk_ordered_sum(x.numel(), _ptr(x), float(scale), _ptr(out), _stream(stream)), "bk_ordered_sum")
+
+
+# Operators around the stage.  Matrices may be views with other columns behind a row (stride(1) = 1).  Tensors that a call
+# cannot take as they are (another dtype or device than it needs, strides it does not know) are refused here, with the status
+# the library itself would give.
+
+def _refuse_unless(ok, where):
+    if not ok:
+        raise BambooError(E_ARG, where)
+
+
+def _rows(t, where, rows=None, cols=None, like=None):
+    """(address, row stride) of a matrix."""
+    _refuse_unless(t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and (rows is None or t.shape[0] == rows) and
+                   (cols is None or t.shape[1] == cols), where)
+    _refuse_unless(t.dtype in _ACT if like is None else t.dtype == like.dtype and t.device == like.device, where)
+    # the stride of a single row says nothing
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _vec(t, n, dtypes, like, where):
+    """Address of n contiguous values, or None."""
+    if t is None:
+        return None
+    _refuse_unless(t.numel() == n and t.is_contiguous() and t.dtype in dtypes and t.device == like.device, where)
+    return t.data_ptr()
+
+
+_ACT = (torch.float32, torch.bfloat16)
+_F32, _I32, _U8 = (torch.float32,), (torch.int32,), (torch.uint8, torch.bool)
+
+
+class _On:
+    """The tensor's device as the current one, and the address of the stream there (the current one if None is given)."""
+
+    def __init__(self, t, stream):
+        self.t, self.stream, self.guard = t, stream, None
+
+    def __enter__(self):
+        if self.t.device.type == "cuda" and self.t.device.index != torch.cuda.current_device():
+            self.guard = torch.cuda.device(self.t.device)
+            self.guard.__enter__()
+        return (self.stream if self.stream is not None else torch.cuda.current_stream()).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _scratch(n, like, stream):
+    """n floats of scratch for one call, held by the allocator until the call's stream is through with it."""
+    t = torch.empty(n, dtype=torch.float32, device=like.device)
+    if stream is not None and stream != torch.cuda.current_stream(like.device):
+        t.record_stream(stream)
+    return t
+
+
+ROTARY_SCALINGS = ("none", "linear", "stretched", "parts")
+
+
+def bk_rotary_frequencies(rot, base=10000.0, scaling="none", factor=1.0, length=0, device="cuda:0"):
+    """(frequencies of the rot/2 pairs as a float64 tensor on `device`, amplitude) for bk_rotary."""
+    _refuse_unless(scaling in ROTARY_SCALINGS and rot >= 2, "bk_rotary_frequencies")
+    freq, amplitude = torch.empty(rot // 2, dtype=torch.float64), C.c_float()
+    _check(lib.bk_rotary_frequencies(rot, base, ROTARY_SCALINGS.index(scaling), factor, length, freq.data_ptr(), C.byref(amplitude)),
+           "bk_rotary_frequencies")
+    return freq.to(device), amplitude.value
+
+
+def bk_rotary(x, freq, y, heads, d, pos=None, seq=1, interleaved=False, inverse=False, amplitude=1.0, stream=None):
+    """y = x with the first 2 * len(freq) features of its first `heads` heads turned by their positions (pos int32 [T], or
+    t mod seq).  y may be x."""
+    where = "bk_rotary"
+    px, ldx = _rows(x, where)
+    py, ldy = _rows(y, where, rows=x.shape[0], like=x)
+    _refuse_unless(min(x.shape[1], y.shape[1]) >= heads * d, where)
+    with _On(x, stream) as s:
+        _check(lib.bk_rotary(_dt(x), x.shape[0], seq, heads, d, 2 * freq.numel(), int(interleaved), int(inverse), px, ldx,
+                             _vec(pos, x.shape[0], _I32, x, where), _vec(freq, freq.numel(), (torch.float64,), x, where),
+                             amplitude, py, ldy, s), where)
+
+
+def _cross_sizes(q, k, batch, heads, kv_heads, where):
+    _refuse_unless(batch > 0 and heads > 0 and kv_heads > 0 and q.dim() == 2 and k.dim() == 2 and q.shape[0] % batch == 0 and
+                   k.shape[0] % batch == 0 and q.shape[1] % heads == 0, where)
+    return q.shape[0] // batch, k.shape[0] // batch, q.shape[1] // heads
+
+
+def bk_cross_attention_fwd(q, k, v, ctx, lse, batch, heads, kv_heads=None, kv_len=None, impl=0, stream=None):
+    """ctx, lse of q [batch*sq, heads*d] over k, v [batch*sk, kv_heads*d]; kv_len: int32 [batch].  Returns the call's scratch."""
+    where = "bk_cross_attention_fwd"
+    kv_heads = heads if kv_heads is None else kv_heads
+    sq, sk, d = _cross_sizes(q, k, batch, heads, kv_heads, where)
+    pq, ldq = _rows(q, where)
+    pk, ldk = _rows(k, where, cols=kv_heads * d, like=q)
+    pv, ldv = _rows(v, where, rows=k.shape[0], cols=kv_heads * d, like=q)
+    pc, ldc = _rows(ctx, where, rows=q.shape[0], cols=q.shape[1], like=q)
+    _refuse_unless(ldk == ldv, where)
+    with _On(q, stream) as s:
+        scratch = _scratch(lib.bk_cross_attention_scratch_floats(batch, sq, sk, heads, kv_heads, d), q, stream)
+        _check(lib.bk_cross_attention_fwd(_dt(q), impl, batch, sq, sk, heads, kv_heads, d, pq, ldq, pk, pv, ldk,
+                                          _vec(kv_len, batch, _I32, q, where), pc, ldc,
+                                          _vec(lse, batch * heads * sq, _F32, q, where), scratch.data_ptr(), s), where)
+    return scratch
+
+
+def bk_cross_attention_bwd(q, k, v, ctx, lse, dctx, dq, dk, dv, batch, heads, kv_heads=None, kv_len=None, impl=0, stream=None):
+    """dq, dk, dv from dctx, with ctx and lse of the forward.  Returns the call's scratch."""
+    where = "bk_cross_attention_bwd"
+    kv_heads = heads if kv_heads is None else kv_heads
+    sq, sk, d = _cross_sizes(q, k, batch, heads, kv_heads, where)
+    pq, ldq = _rows(q, where)
+    (pc, ldc), (pg, ldg), (pdq, lddq) = (_rows(t, where, q.shape[0], q.shape[1], q) for t in (ctx, dctx, dq))
+    (pk, ldk), (pv, ldv), (pdk, lddk), (pdv, lddv) = (_rows(t, where, k.shape[0], kv_heads * d, q) for t in (k, v, dk, dv))
+    _refuse_unless(ldk == ldv and lddk == lddv, where)
+    with _On(q, stream) as s:
+        scratch = _scratch(lib.bk_cross_attention_scratch_floats(batch, sq, sk, heads, kv_heads, d), q, stream)
+        _check(lib.bk_cross_attention_bwd(_dt(q), impl, batch, sq, sk, heads, kv_heads, d, pq, ldq, pk, pv, ldk,
+                                          _vec(kv_len, batch, _I32, q, where), pc, ldc,
+                                          _vec(lse, batch * heads * sq, _F32, q, where), pg, ldg, pdq, lddq, pdk, pdv, lddk,
+                                          scratch.data_ptr(), s), where)
+    return scratch
+
+
+def bk_policy_loss(logits, labels, old_logp, adv, logp, loss_tok, dlogits=None, mask=None, ref_logp=None, kl_tok=None,
+                   entropy=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0, ent_coef=0.0, scale=1.0, stream=None):
+    """Per token: clipped policy loss with a KL and an entropy term, and (dlogits) scale times its gradient."""
+    where = "bk_policy_loss"
+    pl, ldl = _rows(logits, where)
+    T, V = logits.shape
+    pd, ldd = (None, 0) if dlogits is None else _rows(dlogits, where, T, V, logits)
+    f = [_vec(t, T, _F32, logits, where) for t in (old_logp, ref_logp, adv, logp, loss_tok, kl_tok, entropy)]
+    with _On(logits, stream) as s:
+        _check(lib.bk_policy_loss(_dt(logits), T, V, pl, ldl, _vec(labels, T, _I32, logits, where), _vec(mask, T, _U8, logits, where),
+                                  f[0], f[1], f[2], clip_low, clip_high, kl_coef, ent_coef, scale, f[3], f[4], f[5], f[6], pd, ldd,
+                                  s), where)
+
+
+def bk_preference_loss_fwd(logits, labels, ref_logp, lse, logp, logp_seq, margin, loss, beta, smoothing=0.0, mask=None, stream=None):
+    """Per pair: margin and loss; logits of the chosen sequences, then of the rejected ones.  Returns the call's scratch."""
+    where = "bk_preference_loss_fwd"
+    pl, ldl = _rows(logits, where)
+    (T, V), pairs = logits.shape, loss.numel()
+    _refuse_unless(pairs > 0 and T % (2 * pairs) == 0, where)
+    vec = lambda t, n: _vec(t, n, _F32, logits, where)
+    with _On(logits, stream) as s:
+        scratch = _scratch(2 * T, logits, stream)
+        _check(lib.bk_preference_loss_fwd(_dt(logits), pairs, T // (2 * pairs), V, pl, ldl, _vec(labels, T, _I32, logits, where),
+                                          _vec(mask, T, _U8, logits, where), vec(ref_logp, 2 * pairs), beta, smoothing, vec(lse, T),
+                                          vec(logp, T), vec(logp_seq, 2 * pairs), vec(margin, pairs), vec(loss, pairs),
+                                          scratch.data_ptr(), s), where)
+    return scratch
+
+
+def bk_preference_loss_bwd(logits, labels, lse, margin, dlogits, beta, smoothing=0.0, scale=1.0, mask=None, stream=None):
+    """dlogits = scale times the gradient of the pairs' losses."""
+    where = "bk_preference_loss_bwd"
+    pl, ldl = _rows(logits, where)
+    (T, V), pairs = logits.shape, margin.numel()
+    _refuse_unless(pairs > 0 and T % (2 * pairs) == 0, where)
+    pd, ldd = _rows(dlogits, where, T, V, logits)
+    with _On(logits, stream) as s:
+        _check(lib.bk_preference_loss_bwd(_dt(logits), pairs, T // (2 * pairs), V, pl, ldl, _vec(labels, T, _I32, logits, where),
+                                          _vec(mask, T, _U8, logits, where), _vec(lse, T, _F32, logits, where),
+                                          _vec(margin, pairs, _F32, logits, where), beta, smoothing, scale, pd, ldd, s), where)
+
+
+def bk_adamw_group(gs, masters, ms, vs, ws, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, decay=0.0, m_scales=None,
+                   v_scales=None, seed=0, stream=None):
+    """One AdamW step over lists of tensors: fp32 gradients and master weights, moments (fp32, or one-byte codes with fp32
+    scales per 256 elements), storage weights.  decay: a number, or one per tensor."""
+    where, n = "bk_adamw_group", len(masters)
+    eight = m_scales is not None
+    _refuse_unless(n > 0 and len(ws) == n, where)
+    moments = _CODES if eight else _F32
+    lists = [(gs, _F32), (masters, _F32), (ms, moments), (vs, moments), (ws, (ws[0].dtype,))]
+    numel = [t.numel() for t in masters]
+    _refuse_unless(ws[0].dtype in _ACT and (v_scales is not None) == eight, where)
+    decay = [decay] * n if isinstance(decay, (int, float)) else list(decay)
+    _refuse_unless(len(decay) == n, where)
+    device, ptrs = masters[0].device, []
+    for ts, dtypes in lists:
+        _refuse_unless(len(ts) == n, where)
+        for t, k in zip(ts, numel):
+            _refuse_unless(t.numel() == k and t.dtype in dtypes and t.is_contiguous() and t.device == device, where)
+        ptrs.append((_vp * n)(*[t.data_ptr() for t in ts]))
+    for ts in (m_scales, v_scales):
+        if eight:
+            _refuse_unless(len(ts) == n, where)
+            for t, k in zip(ts, numel):
+                _refuse_unless(t.numel() == -(-k // 256) and t.dtype in _F32 and t.is_contiguous() and t.device == device, where)
+        ptrs.append((_vp * n)(*[t.data_ptr() for t in ts]) if eight else None)
+    with _On(masters[0], stream) as s:
+        _check(lib.bk_adamw_group(_dt(ws[0]), 8 if eight else 32, n, (C.c_int64 * n)(*numel), ptrs[0], ptrs[1], ptrs[2], ptrs[3],
+                                  ptrs[5], ptrs[6], ptrs[4], (C.c_double * n)(*decay), lr, beta1, beta2, eps, step, seed & 0xFFFFFFFF, s), where)
+
+
+_CODES = (torch.uint8, torch.float8_e4m3fn)
 
 
 def bk_gemm_stages(n):

@@ -21,7 +21,8 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950", "-Wall", "-Wno-
 # Per-file additions.  The attention kernels do elementwise arithmetic on MFMA results inside their
 # main loops; with the accumulators allocated as ordinary VGPRs (instead of AGPRs) no register moves
 # separate the matrix instructions from that arithmetic.
-EXTRA = {"attention_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+EXTRA = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
+         for f in ("attention_mfma.hip", "cross_attention_mfma.hip", "cross_attention_f32.hip")}
 
 
 def _sources():

@@ -292,6 +292,110 @@ hipError_t launch_ordered_sum(hipStream_t s, long n, const float* in, float scal
 // 907 MB arrays 312 against 278 us.
 inline bool streams_past_cache(long bytes) { return bytes > (384L << 20); }
 
+// ---- operators around the stage ------------------------------------------------------
+// rotary positions: see bk_rotary; tokens, heads_per_wg: what one workgroup takes (set by the launcher)
+struct RotaryDesc {
+  const void* x;
+  void* y;
+  long ldx, ldy;
+  int T, seq, heads, d, rot, neighbours, inverse;
+  int copy;                // 1: y is not x, the features behind rot are passed on
+  const int* pos;          // NULL: position = t mod seq
+  const double* freq;
+  float amplitude;
+  int tokens, heads_per_wg;
+};
+hipError_t launch_rotary(hipStream_t s, int dtype, const RotaryDesc& d);
+
+// losses on given tokens: see bk_policy_loss, bk_preference_loss_fwd / _bwd
+struct PolicyDesc {
+  const void* logits;
+  long ldl;
+  int T, V;
+  const int* labels;
+  const unsigned char* mask;
+  const float *old_logp, *ref_logp, *adv;
+  float clip_low, clip_high, kl_coef, ent_coef, scale;
+  float *logp, *loss_tok, *kl_tok, *entropy;
+  void* dlogits;
+  long ldd;
+};
+hipError_t launch_policy_loss(hipStream_t s, int dtype, const PolicyDesc& d);
+struct PreferenceDesc {
+  const void* logits;
+  long ldl;
+  int pairs, seq, V;
+  const int* labels;
+  const unsigned char* mask;
+  const float* ref_logp;
+  float beta, smoothing, scale;
+  float *lse, *logp, *logp_seq, *margin, *loss;
+  double* scratch;         // [2 * pairs * seq]
+  void* dlogits;
+  long ldd;
+};
+hipError_t launch_preference_fwd(hipStream_t s, int dtype, const PreferenceDesc& d);
+hipError_t launch_preference_bwd(hipStream_t s, int dtype, const PreferenceDesc& d);
+
+// attention over an encoder's states: see bk_cross_attention_fwd / _bwd
+struct CrossDesc {
+  int B, sq, sk, heads, kv_heads, d;
+  const void *q, *k, *v;
+  long ldq, ldkv;
+  const int* kv_len;       // NULL: all keys count
+  void* ctx;               // fwd out / bwd in
+  long ldc;
+  float* lse;              // fwd out / bwd in
+  const void* dctx;
+  long lddc;
+  void *dq, *dk, *dv;
+  long lddq, lddkv;
+  float* scratch;
+  // set by the launchers: rows = sq * group of a (sample, key head) pair, group = heads / kv_heads, group_inv =
+  // ceil(2^32 / group); how many parts the streamed side is cut into, and where the parts' results go
+  int rows, group, splits;
+  unsigned group_inv;
+  float *part, *part_stats, *delta;
+};
+uint64_t cross_attention_scratch_floats(int B, int sq, int sk, int heads, int kv_heads, int d);
+hipError_t launch_cross_attention_fwd(hipStream_t s, int dtype, int impl, const CrossDesc& d);
+hipError_t launch_cross_attention_bwd(hipStream_t s, int dtype, int impl, const CrossDesc& d);
+// the passes, with everything set: bf16 on the matrix cores (head size 64 or 128), and any head size up to 128 in fp32
+// arithmetic on them
+bool cross_mfma_covers(const CrossDesc& d);
+hipError_t launch_cross_fwd_mfma(hipStream_t s, const CrossDesc& d);
+hipError_t launch_cross_dq_mfma(hipStream_t s, const CrossDesc& d);
+hipError_t launch_cross_dkv_mfma(hipStream_t s, const CrossDesc& d);
+hipError_t launch_cross_fwd_f32(hipStream_t s, int dtype, const CrossDesc& d);
+hipError_t launch_cross_dq_f32(hipStream_t s, int dtype, const CrossDesc& d);
+hipError_t launch_cross_dkv_f32(hipStream_t s, int dtype, const CrossDesc& d);
+
+// AdamW on many tensors: see bk_adamw_group
+constexpr int kAdamwTensors = 40;      // of one launch: their descriptors are kernel arguments, 4 KB at most
+struct AdamwTensor {
+  const float* g;
+  float* master;
+  void *m, *v;
+  float *m_scale, *v_scale;
+  void* w;
+  long numel;
+  float keep;              // 1 - lr decay
+  unsigned key;            // of the tensor's rounding
+  int first_wg, aligned;
+};
+struct AdamwBatch {
+  AdamwTensor t[kAdamwTensors];
+  int n;
+  float lr, beta1, beta2, not_beta1, not_beta2, eps, inv_c1, inv_c2;
+};
+static_assert(sizeof(AdamwBatch) <= 4096 - 256, "kernel arguments, with room for the hidden ones");
+struct AdamwHyper {
+  double lr, beta1, beta2, eps;
+  int step;
+};
+hipError_t launch_adamw(hipStream_t s, int dtype, int bits, const AdamwHyper& h, int n, const AdamwTensor* t, const double* decay,
+                        uint32_t seed);
+
 // ---- optimizer ------------------------------------------------------------------
 // Adam on n parameters (n a multiple of 4): fp32 gradient g, fp32 master weights and moments m, v
 // updated in place, w = storage-dtype copy of the new master weights.  step counts from 1.

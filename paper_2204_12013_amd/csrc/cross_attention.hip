@@ -1,0 +1,147 @@
+// Attention over an encoder's states: which kernels run, how many parts the streamed side is cut into, and the launch that
+// joins the parts.
+#include <math.h>
+
+#include "cross_rows.h"
+
+namespace bamboo {
+
+namespace {
+
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Row of `rows` per pair: out = sum of the parts, weighted to their common maximum.  One wavefront a row.
+template <typename T>
+__global__ __launch_bounds__(256) void cross_join_fwd_kernel(CrossDesc a) {
+  const int lane = threadIdx.x & 63;
+  const long n = (long)a.B * a.kv_heads * a.rows, i = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (i >= n) return;
+  const int pair = (int)(i / a.rows), b = pair / a.kv_heads;
+  const CrossRow at = cross_row(a, pair % a.kv_heads, (int)(i % a.rows));
+  float m = -INFINITY;
+  for (int s = 0; s < a.splits; ++s)
+    if (a.part_stats[2 * (s * n + i) + 1] != 0.f) m = fmaxf(m, a.part_stats[2 * (s * n + i)]);     // parts that had keys
+  float l = 0.f, o0 = 0.f, o1 = 0.f;
+  for (int s = 0; s < a.splits; ++s) {
+    const long p = s * n + i;
+    const float ls = a.part_stats[2 * p + 1];
+    if (ls == 0.f) continue;
+    const float w = __builtin_amdgcn_exp2f(a.part_stats[2 * p] - m);
+    l = fmaf(w, ls, l);
+    if (lane < a.d) o0 = fmaf(w, a.part[p * a.d + lane], o0);
+    if (lane + 64 < a.d) o1 = fmaf(w, a.part[p * a.d + lane + 64], o1);
+  }
+  const float inv = l > 0.f ? 1.f / l : l;
+  T* out = (T*)a.ctx + ((long)b * a.sq + at.query) * a.ldc + (long)at.head * a.d;
+  if (lane < a.d) out[lane] = from_f32<T>(o0 * inv);
+  if (lane + 64 < a.d) out[lane + 64] = from_f32<T>(o1 * inv);
+  if (lane == 0) a.lse[cross_stat(a, b, at)] = cross_len(a, b) > 0 ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+}
+
+// Gradients: sums of the parts in order.  One thread an element; KEYS: dk and dv, otherwise dq.
+template <typename T, bool KEYS>
+__global__ __launch_bounds__(256) void cross_join_bwd_kernel(CrossDesc a) {
+  const int per = KEYS ? a.sk : a.rows, cols = KEYS ? 2 * a.d : a.d;
+  const long n = (long)a.B * a.kv_heads * per * cols, i = (long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  float x = 0.f;
+  for (int s = 0; s < a.splits; ++s) x += a.part[s * n + i];
+  const int c = (int)(i % cols);
+  const long row = i / cols;
+  const int pair = (int)(row / per), r = (int)(row % per), b = pair / a.kv_heads, kvh = pair % a.kv_heads;
+  const float scale = rsqrtf((float)a.d);
+  if (KEYS) {
+    const long out = ((long)b * a.sk + r) * a.lddkv + (long)kvh * a.d;
+    if (c < a.d) ((T*)a.dk)[out + c] = from_f32<T>(x * scale);
+    else ((T*)a.dv)[out + c - a.d] = from_f32<T>(x);
+  } else {
+    const CrossRow at = cross_row(a, kvh, r);
+    ((T*)a.dq)[((long)b * a.sq + at.query) * a.lddq + (long)at.head * a.d + c] = from_f32<T>(x * scale);
+  }
+}
+template <bool KEYS>
+hipError_t join_bwd(hipStream_t s, int dtype, const CrossDesc& a) {
+  const long n = (long)a.B * a.kv_heads * (KEYS ? 2L * a.sk : (long)a.rows) * a.d;
+  const dim3 grid((unsigned)((n + 255) / 256));
+  if (dtype == 1) hipLaunchKernelGGL((cross_join_bwd_kernel<bf16_t, KEYS>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((cross_join_bwd_kernel<float, KEYS>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+// Parts of the streamed side (`streamed` rows) for `owned` rows of each of `pairs` problems: one where the owned rows give
+// every CU a workgroup, otherwise as many as make two workgroups a CU, of four tiles at least.
+int parts(long owned, long streamed, long pairs) {
+  const long wgs = (owned + 127) / 128 * pairs, tiles = (streamed + 63) / 64;
+  if (wgs >= 256 || tiles < 8) return 1;
+  long n = (512 + wgs - 1) / wgs;
+  if (n > tiles / 4) n = tiles / 4;
+  return (int)(n < 1 ? 1 : n);
+}
+long up4(long n) { return (n + 3) / 4 * 4; }
+
+struct Plan {
+  int fwd, dq, dkv;                       // parts
+  long fwd_floats, delta, dq_floats, dkv_floats;
+};
+Plan plan(int B, int sq, int sk, int heads, int kv_heads, int d) {
+  const long pairs = (long)B * kv_heads, rows = (long)sq * (heads / kv_heads);
+  Plan p;
+  p.fwd = p.dq = parts(rows, sk, pairs);
+  p.dkv = parts(sk, rows, pairs);
+  p.fwd_floats = p.fwd > 1 ? up4(p.fwd * pairs * rows * d) + up4(p.fwd * pairs * rows * 2) : 0;
+  p.delta = up4(pairs * rows);
+  p.dq_floats = p.dq > 1 ? up4(p.dq * pairs * rows * d) : 0;
+  p.dkv_floats = p.dkv > 1 ? up4(p.dkv * pairs * (long)sk * 2 * d) : 0;
+  return p;
+}
+void shared_fields(CrossDesc& a) {
+  a.group = a.heads / a.kv_heads;
+  a.group_inv = a.group == 1 ? 0 : (unsigned)(((1ull << 32) + a.group - 1) / a.group);
+  a.rows = a.sq * a.group;
+}
+
+}  // namespace
+
+uint64_t cross_attention_scratch_floats(int B, int sq, int sk, int heads, int kv_heads, int d) {
+  const Plan p = plan(B, sq, sk, heads, kv_heads, d);
+  // the parts of one pass after the other in the same place, behind delta
+  const long parts_bwd = p.dq_floats > p.dkv_floats ? p.dq_floats : p.dkv_floats, bwd = p.delta + parts_bwd;
+  return (uint64_t)(p.fwd_floats > bwd ? p.fwd_floats : bwd);
+}
+
+hipError_t launch_cross_attention_fwd(hipStream_t s, int dtype, int impl, const CrossDesc& d) {
+  CrossDesc a = d;
+  shared_fields(a);
+  const Plan p = plan(a.B, a.sq, a.sk, a.heads, a.kv_heads, a.d);
+  a.splits = p.fwd;
+  a.part = a.scratch;
+  a.part_stats = a.scratch + up4(p.fwd * (long)a.B * a.kv_heads * a.rows * a.d);
+  const bool mfma = impl != 1 && dtype == 1 && cross_mfma_covers(a);
+  if (impl == 2 && !mfma) return hipErrorNotSupported;
+  hipError_t e = mfma ? launch_cross_fwd_mfma(s, a) : launch_cross_fwd_f32(s, dtype, a);
+  if (e != hipSuccess || a.splits == 1) return e;
+  const dim3 grid((unsigned)(((long)a.B * a.kv_heads * a.rows + 3) / 4));
+  if (dtype == 1) hipLaunchKernelGGL(cross_join_fwd_kernel<bf16_t>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(cross_join_fwd_kernel<float>, grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_cross_attention_bwd(hipStream_t s, int dtype, int impl, const CrossDesc& d) {
+  CrossDesc a = d;
+  shared_fields(a);
+  const Plan p = plan(a.B, a.sq, a.sk, a.heads, a.kv_heads, a.d);
+  a.delta = a.scratch;
+  a.part = a.scratch + p.delta;
+  const bool mfma = impl != 1 && dtype == 1 && cross_mfma_covers(a);
+  if (impl == 2 && !mfma) return hipErrorNotSupported;
+  a.splits = p.dq;
+  hipError_t e = mfma ? launch_cross_dq_mfma(s, a) : launch_cross_dq_f32(s, dtype, a);
+  if (e == hipSuccess && a.splits > 1) e = join_bwd<false>(s, dtype, a);
+  if (e != hipSuccess) return e;
+  a.splits = p.dkv;
+  e = mfma ? launch_cross_dkv_mfma(s, a) : launch_cross_dkv_f32(s, dtype, a);
+  if (e == hipSuccess && a.splits > 1) e = join_bwd<true>(s, dtype, a);
+  return e;
+}
+
+}  // namespace bamboo

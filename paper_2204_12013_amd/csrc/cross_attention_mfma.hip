@@ -1,0 +1,526 @@
+// Attention over an encoder's states on the matrix cores (bf16 in, fp32 softmax and accumulation), head size 64 or 128.
+//
+// The tiles, their placement in LDS and the operand fragments are those of the self-attention; here the two sides have
+// lengths of their own, keys end at each sample's length, query heads that share a key head are rows of one problem
+// (cross_rows.h), and where the owned rows fill too few workgroups the streamed side is cut into parts whose results are
+// joined by a second launch (the softmax's running maximum and sum make the parts of the forward independent; the
+// gradients are sums).  No atomics: results are bitwise reproducible.
+#include "attention_tiles.h"
+#include "cross_rows.h"
+
+namespace bamboo {
+
+namespace {
+
+// The lane's operand fragments of one row: elements 16 ks + 8 (l / 32) .. + 7, zero where it is not live.
+template <int D>
+__device__ __forceinline__ void lane_row(bf16x8 (&f)[D / 16], const bf16_t* row, bool live) {
+  const int l = threadIdx.x & 63;
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) {
+    bf16x8 t = {};
+    if (live) t = *(const bf16x8*)(row + ks * 16 + (l >> 5) * 8);
+    f[ks] = t;
+  }
+}
+// A wavefront's transposed result (lane = row) through its private LDS area to rows wherever `at` says they are.
+template <int D, typename AT>
+__device__ __forceinline__ void put_rows(const f32x16 (&acc)[D / 32], float mul, bf16_t* stage, int row0, int row_lim, AT at) {
+  constexpr int LD = D + 8;
+  const int l = threadIdx.x & 63;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+      bf16x4 o;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[c] = (bf16_t)(acc[dt][4 * a + c] * mul);
+      *(bf16x4*)(stage + (l & 31) * LD + dt * 32 + 8 * a + 4 * (l >> 5)) = o;
+    }
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int it = 0; it < 32 * (D / 8) / 64; ++it) {
+    const int idx = l + it * 64;
+    const int row = idx / (D / 8), ch = (idx % (D / 8)) * 8;
+    const bf16x8 t = *(const bf16x8*)(stage + row * LD + ch);
+    if (row0 + row < row_lim) *(bf16x8*)(at(row0 + row) + ch) = t;
+  }
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  __builtin_amdgcn_wave_barrier();
+}
+// the lane's row of a part's result, unscaled
+template <int D>
+__device__ __forceinline__ void put_part(const f32x16 (&acc)[D / 32], float* row) {
+  const int g = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+      f32x4 t;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) t[c] = acc[dt][4 * a + c];
+      *(f32x4*)(row + dt * 32 + 8 * a + 4 * g) = t;
+    }
+}
+template <int N> __device__ __forceinline__ void clear(f32x16 (&x)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[i][r] = 0.f;
+}
+
+// -------------------------------------------------------------------------------------------- forward
+template <int D>
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cross_fwd_mfma_kernel(CrossDesc a) {
+  constexpr unsigned TB = TileCopy<D>::BYTES;
+  extern __shared__ __attribute__((aligned(256))) unsigned char smem_raw[];
+  const unsigned ring = lds_address(smem_raw);    // [2][keys, values]
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 5;
+  const CrossBlock w = cross_block(a);
+  const int len = __builtin_amdgcn_readfirstlane(cross_len(a, w.b));
+  int t0, t1;
+  cross_part(len, a.splits, w.split, &t0, &t1);
+  const int nt = t1 - t0;
+  const int qw0 = w.blk * 128 + wave * 32, row = qw0 + (lane & 31);
+  const bool live = row < a.rows, busy = qw0 < a.rows;
+  const CrossRow at = cross_row(a, w.kvh, min(row, a.rows - 1));
+  const bf16_t* kb = (const bf16_t*)a.k + (long)w.b * a.sk * a.ldkv + w.kvh * D;
+  const bf16_t* vb = (const bf16_t*)a.v + (long)w.b * a.sk * a.ldkv + w.kvh * D;
+  const float c = rsqrtf((float)D) * kLog2e;
+
+  bf16x8 qf[D / 16];
+  lane_row<D>(qf, (const bf16_t*)a.q + ((long)w.b * a.sq + at.query) * a.ldq + at.head * D, live);
+  f32x16 o[D / 32];
+  clear(o);
+  float m_i = kMasked, l_i = 0.f;
+  TileCopy<D> copy;
+  copy.init(a.ldkv, max(len, 1));
+  FragAddr<D, true> fr;
+  fr.init(ring);
+  if (nt > 0) {
+    copy.issue(kb, t0, ring);
+    copy.issue(vb, t0, ring + TB);
+  }
+  for_each_tile(nt, [&](int t, int slot) __attribute__((always_inline)) {
+    const unsigned buf = slot * 2 * TB;
+    wait_tiles<0>();
+    __syncthreads();                              // tile t is there, and tile t - 1 has been read everywhere
+    if (t + 1 < nt) {
+      const unsigned ring = lds_address(smem_raw);
+      copy.issue(kb, t0 + t + 1, ring + (slot ^ 1) * 2 * TB);
+      copy.issue(vb, t0 + t + 1, ring + (slot ^ 1) * 2 * TB + TB);
+    }
+    if (busy) {                                   // uniform over the wavefront
+      const int k0 = (t0 + t) * TILE;
+      f32x16 s[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[u][r] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_k(buf, 0, u * 32, ks), qf[ks], s[u], 0, 0, 0);
+      // Online softmax in the log2 domain.  The running maximum is raised only where some row's has grown by more than 8
+      // (a factor of 256, harmless in fp32 and bf16): the output is rescaled on a few tiles instead of on every one.
+      if (k0 + TILE > len) {                      // the last tile: keys behind the length
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[u][r] = k0 + u * 32 + acc_row(r) < len ? s[u][r] : kMasked;
+      }
+      float mx = kMasked;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[u][r]);
+      mx *= c;
+      mx = fmaxf(mx, other_half(mx));
+      const bool grow = mx > m_i + 8.f;
+      if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+        const float m_new = grow ? mx : m_i;
+        const float alpha = __builtin_amdgcn_exp2f(m_i - m_new);
+        l_i *= alpha;
+        m_i = m_new;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[dt][r] *= alpha;
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[u][r] = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -m_i));
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const bf16x8 pb = pack8(s[u >> 1], u & 1);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) l_i += s[u >> 1][8 * (u & 1) + j];
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+          o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_tr(buf, TB, dt, 16 * u), pb, o[dt], 0, 0, 0);
+      }
+    }
+  });
+  __syncthreads();                                // the tiles' place takes the results
+  const float l_tot = l_i + other_half(l_i);
+  if (a.splits > 1) {
+    if (!live) return;
+    const long i = ((long)w.split * a.B * a.kv_heads + w.pair) * a.rows + row;
+    put_part<D>(o, a.part + i * D);
+    if (g == 0) {
+      a.part_stats[2 * i] = m_i;
+      a.part_stats[2 * i + 1] = l_tot;
+    }
+    return;
+  }
+  bf16_t* stage = (bf16_t*)smem_raw + wave * 32 * (D + 8);
+  put_rows<D>(o, l_tot > 0.f ? 1.f / l_tot : l_tot, stage, qw0, a.rows, [&](int r) {
+    const CrossRow p = cross_row(a, w.kvh, r);
+    return (bf16_t*)a.ctx + ((long)w.b * a.sq + p.query) * a.ldc + p.head * D;
+  });
+  if (g == 0 && live) a.lse[cross_stat(a, w.b, at)] = len > 0 ? (m_i + __builtin_amdgcn_logf(l_tot)) * kLn2 : -INFINITY;
+}
+
+// ------------------------------------------------------------------------------------------- backward
+// Owns rows, streams keys.
+template <int D>
+__global__ __launch_bounds__(256, 2) void cross_dq_mfma_kernel(CrossDesc a) {
+  constexpr unsigned TB = TileCopy<D>::BYTES;
+  extern __shared__ __attribute__((aligned(256))) unsigned char smem_raw[];
+  const unsigned ring = lds_address(smem_raw);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const CrossBlock w = cross_block(a);
+  const int len = __builtin_amdgcn_readfirstlane(cross_len(a, w.b));
+  int t0, t1;
+  cross_part(len, a.splits, w.split, &t0, &t1);
+  const int nt = t1 - t0;
+  const int qw0 = w.blk * 128 + wave * 32, row = qw0 + (lane & 31);
+  const bool live = row < a.rows, busy = qw0 < a.rows;
+  const CrossRow at = cross_row(a, w.kvh, min(row, a.rows - 1));
+  const long tok = (long)w.b * a.sq + at.query, stat = cross_stat(a, w.b, at);
+  const bf16_t* kb = (const bf16_t*)a.k + (long)w.b * a.sk * a.ldkv + w.kvh * D;
+  const bf16_t* vb = (const bf16_t*)a.v + (long)w.b * a.sk * a.ldkv + w.kvh * D;
+  const float scale = rsqrtf((float)D), c = scale * kLog2e;
+
+  bf16x8 qf[D / 16], dof[D / 16];
+  lane_row<D>(qf, (const bf16_t*)a.q + tok * a.ldq + at.head * D, live);
+  lane_row<D>(dof, (const bf16_t*)a.dctx + tok * a.lddc + at.head * D, live);
+  const float lse2 = a.lse[stat] * kLog2e;
+  float delta = 0.f;                              // rowsum(ctx * dctx)
+  {
+    bf16x8 of[D / 16];
+    lane_row<D>(of, (const bf16_t*)a.ctx + tok * a.ldc + at.head * D, live);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) delta += (float)of[ks][j] * (float)dof[ks][j];
+    delta += other_half(delta);
+  }
+  f32x16 dq[D / 32];
+  clear(dq);
+  FragAddr<D, false> fr;
+  fr.init(0);
+  TileCopy<D> copy;
+  copy.init(a.ldkv, max(len, 1));
+  if (nt > 0) {
+    copy.issue(kb, t0, ring);
+    copy.issue(vb, t0, ring + TB);
+  }
+  const f32x16 zero16 = {};
+  if (a.splits == 1 && nt > 0 && nt <= 2) {
+    // Few keys: both tiles fit the ring, and delta is the sum of p dP as the scores give it.  ctx has been rounded to bf16, and
+    // what that is off by does not average out over few keys (error of dQ: 3 keys 0.0043 of its norm, 0.0024 this way; at
+    // 333 keys the roundings of dS and dQ themselves are 0.0024 and those of delta 0.0007).
+    if (nt == 2) {
+      copy.issue(kb, t0 + 1, ring + 2 * TB);
+      copy.issue(vb, t0 + 1, ring + 3 * TB);
+    }
+    wait_tiles<0>();
+    __syncthreads();
+    delta = 0.f;
+    if (busy)
+      for (int t = 0; t < nt; ++t) {
+        const unsigned buf = ring + t * 2 * TB;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          f32x16 s = zero16, dp = zero16;
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks) {
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_k(buf, 0, u * 32, ks), qf[ks], s, 0, 0, 0);
+            dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_k(buf, TB, u * 32, ks), dof[ks], dp, 0, 0, 0);
+          }
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if ((t0 + t) * TILE + u * 32 + acc_row(r) < len) delta = fmaf(__builtin_amdgcn_exp2f(fmaf(s[r], c, -lse2)), dp[r], delta);
+        }
+      }
+    delta += other_half(delta);
+  }
+  if (lane < 32 && live && w.split == 0) a.delta[stat] = delta;
+  f32x16 neg_delta;                               // the dP products start from -delta
+#pragma unroll
+  for (int r = 0; r < 16; ++r) neg_delta[r] = -delta;
+  wait_tiles<0>();
+  __syncthreads();
+  for (int t = 0; t < nt; ++t) {
+    const int slot = t & 1;
+    const unsigned buf = ring + slot * 2 * TB;
+    const int k0 = (t0 + t) * TILE;
+    if (t + 1 < nt) {
+      copy.issue(kb, t0 + t + 1, ring + (slot ^ 1) * 2 * TB);
+      copy.issue(vb, t0 + t + 1, ring + (slot ^ 1) * 2 * TB + TB);
+    }
+    if (busy) {
+      f32x16 s[2], dp[2];
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_k(buf, 0, u * 32, ks), qf[ks], ks == 0 ? zero16 : s[u], 0, 0, 0);
+          dp[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_k(buf, TB, u * 32, ks), dof[ks], ks == 0 ? neg_delta : dp[u], 0,
+                                                          0, 0);
+        }
+      if (k0 + TILE > len) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -lse2));
+            s[u][r] = k0 + u * 32 + acc_row(r) < len ? p * dp[u][r] : 0.f;       // dS^T
+          }
+      } else {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[u][r] = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -lse2)) * dp[u][r];
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const bf16x8 dsb = pack8(s[u >> 1], u & 1);
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+          dq[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_tr(buf, 0, dt, 16 * u), dsb, dq[dt], 0, 0, 0);
+      }
+    }
+    wait_tiles<0>();
+    __syncthreads();
+  }
+  if (a.splits > 1) {
+    if (live) put_part<D>(dq, a.part + (((long)w.split * a.B * a.kv_heads + w.pair) * a.rows + row) * D);
+    return;
+  }
+  bf16_t* stage = (bf16_t*)smem_raw + wave * 32 * (D + 8);
+  put_rows<D>(dq, scale, stage, qw0, a.rows, [&](int r) {
+    const CrossRow p = cross_row(a, w.kvh, r);
+    return (bf16_t*)a.dq + ((long)w.b * a.sq + p.query) * a.lddq + p.head * D;
+  });
+}
+
+// Rows of the pair, 64 to a tile, from wherever their query and head are.  Offsets in 32 bits: see covers().
+template <int D>
+struct RowCopy {
+  static constexpr int N = TileCopy<D>::N;
+  unsigned col[N];
+  unsigned wave_lds;
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = threadIdx.x + i * 256, r = c / (D / 8);
+      col[i] = (unsigned)(((c % (D / 8)) ^ swz<D>(r)) * 8) * 2u;
+    }
+    wave_lds = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
+  }
+  // the same rows of two tensors
+  __device__ __forceinline__ void issue(const CrossDesc& a, const bf16_t* g0, long ld0, unsigned lds0, const bf16_t* g1, long ld1,
+                                        unsigned lds1, int tile) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = min(tile * TILE + (int)(threadIdx.x + i * 256) / (D / 8), a.rows - 1);
+      const CrossRow p = cross_row(a, 0, r);
+      const unsigned in_row = (unsigned)p.head * (D * 2) + col[i];
+      asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+                   :
+                   : "v"((unsigned)p.query * (unsigned)(ld0 * 2) + in_row), "s"(g0), "s"(lds0 + wave_lds + i * 4096)
+                   : "memory", "m0");
+      asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+                   :
+                   : "v"((unsigned)p.query * (unsigned)(ld1 * 2) + in_row), "s"(g1), "s"(lds1 + wave_lds + i * 4096)
+                   : "memory", "m0");
+    }
+  }
+};
+
+// Owns keys, streams rows.
+template <int D>
+__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void cross_dkv_mfma_kernel(CrossDesc a) {
+  constexpr unsigned TB = TileCopy<D>::BYTES;
+  extern __shared__ __attribute__((aligned(256))) unsigned char smem_raw[];
+  const unsigned ring = lds_address(smem_raw);    // [2][queries, gradients]
+  float* lse_s = (float*)(smem_raw + 4 * TB);     // [2][64] (log2 domain), behind the tiles
+  float* del_s = lse_s + 2 * TILE;                // [2][64]
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 5;
+  const CrossBlock w = cross_block(a);
+  const int len = __builtin_amdgcn_readfirstlane(cross_len(a, w.b));
+  const int kw0 = w.blk * 128 + wave * 32, key = kw0 + (lane & 31);
+  int t0, t1;
+  cross_part(a.rows, a.splits, w.split, &t0, &t1);
+  const int nt = w.blk * 128 < len ? t1 - t0 : 0;
+  const bool busy = kw0 < len;
+  const bf16_t* qb = (const bf16_t*)a.q + (long)w.b * a.sq * a.ldq + w.kvh * a.group * D;
+  const bf16_t* gb = (const bf16_t*)a.dctx + (long)w.b * a.sq * a.lddc + w.kvh * a.group * D;
+  const float scale = rsqrtf((float)D), c = scale * kLog2e;
+
+  bf16x8 kf[D / 16], vf[D / 16];
+  const long at_key = ((long)w.b * a.sk + min(key, a.sk - 1)) * a.ldkv + w.kvh * D;
+  lane_row<D>(kf, (const bf16_t*)a.k + at_key, key < len);
+  lane_row<D>(vf, (const bf16_t*)a.v + at_key, key < len);
+  f32x16 dk[D / 32], dv[D / 32];
+  clear(dk);
+  clear(dv);
+  float lse_r = 0.f, del_r = 0.f;
+  auto fetch_stats = [&](int r0) {
+    if (threadIdx.x < TILE) {
+      const int r = r0 + threadIdx.x;
+      const long stat = cross_stat(a, w.b, cross_row(a, w.kvh, min(r, a.rows - 1)));
+      lse_r = a.lse[stat] * kLog2e;
+      del_r = -a.delta[stat];                     // negated: the dP accumulators start from it
+    }
+  };
+  auto stash_stats = [&](int buf) {
+    if (threadIdx.x < TILE) {
+      lse_s[buf * TILE + threadIdx.x] = lse_r;
+      del_s[buf * TILE + threadIdx.x] = del_r;
+    }
+  };
+  FragAddr<D, false> fr;
+  fr.init(0);
+  RowCopy<D> copy;
+  copy.init();
+  if (nt > 0) {
+    copy.issue(a, qb, a.ldq, ring, gb, a.lddc, ring + TB, t0);
+    fetch_stats(t0 * TILE);
+    stash_stats(0);
+  }
+  wait_tiles<0>();
+  __syncthreads();
+  for (int t = 0; t < nt; ++t) {
+    const int slot = t & 1;
+    const unsigned buf = ring + slot * 2 * TB;
+    const int r0 = (t0 + t) * TILE;
+    if (t + 1 < nt) {
+      fetch_stats(r0 + TILE);
+      copy.issue(a, qb, a.ldq, ring + (slot ^ 1) * 2 * TB, gb, a.lddc, ring + (slot ^ 1) * 2 * TB + TB, t0 + t + 1);
+    }
+    if (busy) {
+      f32x16 s[2], dp[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int a4 = 0; a4 < 4; ++a4) {
+          const f32x4 d4 = *(const f32x4*)(del_s + slot * TILE + u * 32 + 8 * a4 + 4 * g);
+#pragma unroll
+          for (int cc = 0; cc < 4; ++cc) dp[u][4 * a4 + cc] = d4[cc];
+        }
+      const f32x16 zero16 = {};
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_k(buf, 0, u * 32, ks), kf[ks], ks == 0 ? zero16 : s[u], 0, 0, 0);
+          dp[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_k(buf, TB, u * 32, ks), vf[ks], dp[u], 0, 0, 0);
+        }
+      const bool need_mask = (r0 + TILE > a.rows) || (kw0 + 32 > len);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int a4 = 0; a4 < 4; ++a4) {
+          const int first = u * 32 + 8 * a4 + 4 * g;   // of 4 consecutive rows of this lane
+          const f32x4 l4 = *(const f32x4*)(lse_s + slot * TILE + first);
+          if (need_mask) {                             // uniform over the wavefront
+#pragma unroll
+            for (int cc = 0; cc < 4; ++cc) {
+              const int r = 4 * a4 + cc;
+              const bool counts = r0 + first + cc < a.rows && key < len;
+              const float p = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -l4[cc]));
+              s[u][r] = counts ? p : 0.f;
+              dp[u][r] = counts ? dp[u][r] * p : 0.f;  // dS
+            }
+          } else {
+#pragma unroll
+            for (int cc = 0; cc < 4; ++cc) {
+              const int r = 4 * a4 + cc;
+              const float p = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -l4[cc]));
+              s[u][r] = p;
+              dp[u][r] *= p;
+            }
+          }
+        }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const bf16x8 pb = pack8(s[u >> 1], u & 1);
+        const bf16x8 dsb = pack8(dp[u >> 1], u & 1);
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) {
+          dv[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_tr(buf, TB, dt, 16 * u), pb, dv[dt], 0, 0, 0);
+          dk[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_tr(buf, 0, dt, 16 * u), dsb, dk[dt], 0, 0, 0);
+        }
+      }
+    }
+    if (t + 1 < nt) stash_stats(slot ^ 1);
+    wait_tiles<0>();
+    __syncthreads();
+  }
+  if (a.splits > 1) {
+    if (key < a.sk) {
+      float* out = a.part + (((long)w.split * a.B * a.kv_heads + w.pair) * a.sk + key) * (2 * D);
+      put_part<D>(dk, out);
+      put_part<D>(dv, out + D);
+    }
+    return;
+  }
+  bf16_t* stage = (bf16_t*)smem_raw + wave * 32 * (D + 8);
+  const long out = (long)w.b * a.sk * a.lddkv + w.kvh * D;
+  put_rows<D>(dk, scale, stage, kw0, a.sk, [&](int r) { return (bf16_t*)a.dk + out + (long)r * a.lddkv; });
+  put_rows<D>(dv, 1.f, stage, kw0, a.sk, [&](int r) { return (bf16_t*)a.dv + out + (long)r * a.lddkv; });
+}
+
+enum { FWD, DQ, DKV };
+template <int D, int PASS>
+hipError_t launch(hipStream_t s, const CrossDesc& a) {
+  constexpr int BYTES = 4 * TileCopy<D>::BYTES + (PASS == DKV ? 4 * TILE * 4 : 0);
+  static_assert(BYTES >= 4 * 32 * (D + 8) * 2, "the four staging areas");
+  constexpr auto kern = PASS == FWD ? cross_fwd_mfma_kernel<D> : (PASS == DQ ? cross_dq_mfma_kernel<D> : cross_dkv_mfma_kernel<D>);
+  const hipError_t e = ensure_lds_attribute<kern, BYTES>();
+  if (e != hipSuccess) return e;
+  const unsigned grid = (unsigned)(((PASS == DKV ? a.sk : a.rows) + 127) / 128) * a.splits * a.B * a.kv_heads;
+  hipLaunchKernelGGL(kern, dim3(grid), dim3(256), BYTES, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+bool cross_mfma_covers(const CrossDesc& a) {
+  if (a.d != 64 && a.d != 128) return false;
+  uintptr_t bits = 0;
+  for (const void* p : {a.q, a.k, a.v, (const void*)a.ctx, a.dctx, (const void*)a.dq, (const void*)a.dk, (const void*)a.dv})
+    bits |= (uintptr_t)p;
+  const long lds = a.ldq | a.ldkv | a.ldc | a.lddc | a.lddq | a.lddkv;
+  if (lds % 8 || bits & 15) return false;
+  // byte offsets inside one sample are 32-bit, those of the rows of a last, partial tile included (they are clamped after the add)
+  const long widest = 1L << 32;
+  return ((long)a.sk + TILE) * a.ldkv * 2 < widest && (long)a.sq * a.ldq * 2 < widest && (long)a.sq * a.lddc * 2 < widest;
+}
+hipError_t launch_cross_fwd_mfma(hipStream_t s, const CrossDesc& a) {
+  return a.d == 64 ? launch<64, FWD>(s, a) : launch<128, FWD>(s, a);
+}
+hipError_t launch_cross_dq_mfma(hipStream_t s, const CrossDesc& a) {
+  return a.d == 64 ? launch<64, DQ>(s, a) : launch<128, DQ>(s, a);
+}
+hipError_t launch_cross_dkv_mfma(hipStream_t s, const CrossDesc& a) {
+  return a.d == 64 ? launch<64, DKV>(s, a) : launch<128, DKV>(s, a);
+}
+
+}  // namespace bamboo

@@ -1,7 +1,13 @@
 // C ABI of the individual kernels: argument checks and marshalling only.
+#include <math.h>
 #include <stdio.h>
 #include <stdlib.h>
 #include <string.h>
+
+#include <algorithm>
+#include <new>
+#include <utility>
+#include <vector>
 
 #include "../../include/bamboo_debug.h"
 #include "../../include/bamboo_kernels.h"
@@ -223,6 +229,211 @@ int bk_ordered_sum(int64_t n, const float* in, float scale, float* out, void* st
   if (n <= 0 || !in || !out) return BAMBOO_E_ARG;
   (void)hipGetLastError();
   return finish(launch_ordered_sum((hipStream_t)stream, (long)n, in, scale, out));
+}
+
+// ---- operators around the stage ----------------------------------------------
+
+// rows of `cols` elements of `es` bytes, ld elements apart
+struct Span { uintptr_t first, last; };
+static Span span_of(const void* p, int64_t rows, int64_t ld, int64_t cols, int es) {
+  return {(uintptr_t)p, (uintptr_t)p + (uintptr_t)(((rows - 1) * ld + cols) * es)};
+}
+// an output that may be its input, row on row, but not lie across it
+static bool lies_across(const Span& in, const Span& out, bool same_rows) {
+  if (out.first >= in.last || in.first >= out.last) return false;
+  return !(same_rows && in.first == out.first);
+}
+static int element_size(int dtype) { return dtype == 1 ? 2 : 4; }
+static bool element_aligned(int dtype, const void* p) { return ((uintptr_t)p & (element_size(dtype) - 1)) == 0; }
+
+int bk_rotary(int dtype, int T, int seq, int heads, int d, int rot, int interleaved, int inverse, const void* x,
+              int64_t ldx, const int32_t* pos, const double* freq, float amplitude, void* y, int64_t ldy, void* stream) {
+  if ((dtype != 0 && dtype != 1) || T <= 0 || heads <= 0 || d < 2 || d > 512 || rot < 2 || rot > d || rot % 2) return BAMBOO_E_ARG;
+  if (!x || !y || !freq || (!pos && seq <= 0)) return BAMBOO_E_ARG;
+  const int64_t cols = (int64_t)heads * d;
+  if (cols > 0x7fffffff / 8 || ldx < cols || ldy < cols || !element_aligned(dtype, x) || !element_aligned(dtype, y)) return BAMBOO_E_ARG;
+  const int es = element_size(dtype);
+  if (lies_across(span_of(x, T, ldx, cols, es), span_of(y, T, ldy, cols, es), ldx == ldy)) return BAMBOO_E_ARG;
+  RotaryDesc a;
+  memset(&a, 0, sizeof(a));
+  a.x = x; a.y = y; a.ldx = ldx; a.ldy = ldy; a.T = T; a.seq = seq; a.heads = heads; a.d = d; a.rot = rot;
+  a.neighbours = interleaved != 0; a.inverse = inverse != 0; a.copy = x != y; a.pos = pos; a.freq = freq; a.amplitude = amplitude;
+  (void)hipGetLastError();
+  return finish(launch_rotary((hipStream_t)stream, dtype, a));
+}
+
+int bk_rotary_frequencies(int rot, double base, int scaling, double factor, int length, double* freq, float* amplitude) {
+  if (rot < 2 || rot % 2 || !(base > 1.) || scaling < 0 || scaling > 3 || !freq) return BAMBOO_E_ARG;
+  if (!(base < INFINITY) || (scaling != 0 && !(factor >= 1. && factor < INFINITY)) || (scaling == 3 && length <= 0)) return BAMBOO_E_ARG;
+  if (scaling == 2 && rot > 2) base *= pow(factor, (double)rot / (rot - 2));
+  for (int i = 0; i < rot / 2; ++i) {
+    double f = pow(base, -2. * i / rot);
+    if (scaling == 1) f /= factor;
+    if (scaling == 3) {
+      const double turns = length * f / 6.283185307179586477, kept = fmin(1., fmax(0., (turns - 1.) / 31.));
+      f *= kept + (1. - kept) / factor;
+    }
+    freq[i] = f;
+  }
+  if (amplitude) *amplitude = scaling == 3 ? (float)(0.1 * log(factor) + 1.) : 1.f;
+  return BAMBOO_OK;
+}
+
+static int cross_desc(CrossDesc& a, int dtype, int impl, int batch, int sq, int sk, int heads, int kv_heads, int d, const void* q,
+                      int64_t ldq, const void* k, const void* v, int64_t ldkv, const int32_t* kv_len, const void* ctx, int64_t ldc,
+                      const float* lse, float* scratch) {
+  if ((dtype != 0 && dtype != 1) || impl < 0 || impl > 2 || batch <= 0 || sq <= 0 || sk <= 0 || heads <= 0 || kv_heads <= 0 ||
+      heads % kv_heads || d <= 0 || d > 128)
+    return BAMBOO_E_ARG;
+  if (!q || !k || !v || !ctx || !lse) return BAMBOO_E_ARG;
+  for (const void* p : {q, k, v, ctx})
+    if (!element_aligned(dtype, p)) return BAMBOO_E_ARG;
+  if (ldq < (int64_t)heads * d || ldkv < (int64_t)kv_heads * d || ldc < (int64_t)heads * d) return BAMBOO_E_ARG;
+  // row numbers and workgroups are 32-bit
+  const int64_t group = heads / kv_heads, rows = sq * group, pairs = (int64_t)batch * kv_heads;
+  const int64_t most = rows > sk ? rows : sk;
+  if (rows > 0x7fffff00 || rows * group > 0xffffffffLL || sk > 0x7fffff00 || pairs > 0x7fffffff ||
+      (most / 4 + 1024) * pairs > 0x7fffffff || pairs * most * 2 * d / 256 + 1 > 0x7fffffff)
+    return BAMBOO_E_ARG;
+  if ((!scratch && bk_cross_attention_scratch_floats(batch, sq, sk, heads, kv_heads, d) > 0) || ((uintptr_t)scratch & 15)) return BAMBOO_E_ARG;
+  memset(&a, 0, sizeof(a));
+  a.B = batch; a.sq = sq; a.sk = sk; a.heads = heads; a.kv_heads = kv_heads; a.d = d;
+  a.q = q; a.k = k; a.v = v; a.ldq = ldq; a.ldkv = ldkv; a.kv_len = kv_len;
+  a.ctx = (void*)ctx; a.ldc = ldc; a.lse = (float*)lse; a.scratch = scratch;
+  return BAMBOO_OK;
+}
+
+uint64_t bk_cross_attention_scratch_floats(int batch, int sq, int sk, int heads, int kv_heads, int d) {
+  if (batch <= 0 || sq <= 0 || sk <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || d <= 0 || d > 128) return 0;
+  return cross_attention_scratch_floats(batch, sq, sk, heads, kv_heads, d);
+}
+
+int bk_cross_attention_fwd(int dtype, int impl, int batch, int sq, int sk, int heads, int kv_heads, int d, const void* q,
+                           int64_t ldq, const void* k, const void* v, int64_t ldkv, const int32_t* kv_len, void* ctx,
+                           int64_t ldc, float* lse, float* scratch, void* stream) {
+  CrossDesc a;
+  const int rc = cross_desc(a, dtype, impl, batch, sq, sk, heads, kv_heads, d, q, ldq, k, v, ldkv, kv_len, ctx, ldc, lse, scratch);
+  if (rc != BAMBOO_OK) return rc;
+  (void)hipGetLastError();
+  return finish(launch_cross_attention_fwd((hipStream_t)stream, dtype, impl, a));
+}
+
+int bk_cross_attention_bwd(int dtype, int impl, int batch, int sq, int sk, int heads, int kv_heads, int d, const void* q,
+                           int64_t ldq, const void* k, const void* v, int64_t ldkv, const int32_t* kv_len,
+                           const void* ctx, int64_t ldc, const float* lse, const void* dctx, int64_t lddc, void* dq,
+                           int64_t lddq, void* dk, void* dv, int64_t lddkv, float* scratch, void* stream) {
+  CrossDesc a;
+  const int rc = cross_desc(a, dtype, impl, batch, sq, sk, heads, kv_heads, d, q, ldq, k, v, ldkv, kv_len, ctx, ldc, lse, scratch);
+  if (rc != BAMBOO_OK) return rc;
+  if (!dctx || !dq || !dk || !dv || lddc < (int64_t)heads * d || lddq < (int64_t)heads * d || lddkv < (int64_t)kv_heads * d)
+    return BAMBOO_E_ARG;
+  for (const void* p : {dctx, (const void*)dq, (const void*)dk, (const void*)dv})
+    if (!element_aligned(dtype, p)) return BAMBOO_E_ARG;
+  a.dctx = dctx; a.lddc = lddc; a.dq = dq; a.lddq = lddq; a.dk = dk; a.dv = dv; a.lddkv = lddkv;
+  (void)hipGetLastError();
+  return finish(launch_cross_attention_bwd((hipStream_t)stream, dtype, impl, a));
+}
+
+// the gradient's buffer: whole elements, and either the logits' own rows or none of them
+static bool bad_gradient(int dtype, int64_t rows, int V, const void* logits, int64_t ldl, const void* dlogits, int64_t ldd) {
+  const int es = element_size(dtype);
+  return ldd < V || !element_aligned(dtype, dlogits) ||
+         lies_across(span_of(logits, rows, ldl, V, es), span_of(dlogits, rows, ldd, V, es), ldl == ldd);
+}
+
+int bk_policy_loss(int dtype, int T, int V, const void* logits, int64_t ldl, const int32_t* labels, const uint8_t* mask,
+                   const float* old_logp, const float* ref_logp, const float* adv, float clip_low, float clip_high,
+                   float kl_coef, float ent_coef, float scale, float* logp, float* loss_tok, float* kl_tok,
+                   float* entropy, void* dlogits, int64_t ldd, void* stream) {
+  if ((dtype != 0 && dtype != 1) || T <= 0 || V <= 0 || V > 0x7fff0000 || ldl < V) return BAMBOO_E_ARG;
+  if (!logits || !labels || !old_logp || !adv || !logp || !loss_tok || !element_aligned(dtype, logits)) return BAMBOO_E_ARG;
+  if (!(clip_low >= 0.f && clip_low <= 1.f && clip_high >= 0.f)) return BAMBOO_E_ARG;
+  if (dlogits && bad_gradient(dtype, T, V, logits, ldl, dlogits, ldd)) return BAMBOO_E_ARG;
+  PolicyDesc a;
+  memset(&a, 0, sizeof(a));
+  a.logits = logits; a.ldl = ldl; a.T = T; a.V = V; a.labels = labels; a.mask = mask; a.old_logp = old_logp; a.ref_logp = ref_logp;
+  a.adv = adv; a.clip_low = clip_low; a.clip_high = clip_high; a.kl_coef = kl_coef; a.ent_coef = ent_coef; a.scale = scale;
+  a.logp = logp; a.loss_tok = loss_tok; a.kl_tok = kl_tok; a.entropy = entropy; a.dlogits = dlogits; a.ldd = ldd;
+  (void)hipGetLastError();
+  return finish(launch_policy_loss((hipStream_t)stream, dtype, a));
+}
+
+static int preference_desc(PreferenceDesc& a, int dtype, int pairs, int seq, int V, const void* logits, int64_t ldl,
+                           const int32_t* labels, const uint8_t* mask, float beta, float smoothing) {
+  if ((dtype != 0 && dtype != 1) || pairs <= 0 || seq <= 0 || V <= 0 || V > 0x7fff0000 || ldl < V) return BAMBOO_E_ARG;
+  if ((int64_t)2 * pairs * seq > 0x7fffffff || !logits || !labels || !element_aligned(dtype, logits)) return BAMBOO_E_ARG;
+  if (!(smoothing >= 0.f && smoothing <= 1.f)) return BAMBOO_E_ARG;
+  memset(&a, 0, sizeof(a));
+  a.logits = logits; a.ldl = ldl; a.pairs = pairs; a.seq = seq; a.V = V; a.labels = labels; a.mask = mask; a.beta = beta;
+  a.smoothing = smoothing;
+  return BAMBOO_OK;
+}
+
+int bk_preference_loss_fwd(int dtype, int pairs, int seq, int V, const void* logits, int64_t ldl, const int32_t* labels,
+                           const uint8_t* mask, const float* ref_logp, float beta, float smoothing, float* lse,
+                           float* logp, float* logp_seq, float* margin, float* loss, double* scratch, void* stream) {
+  PreferenceDesc a;
+  const int rc = preference_desc(a, dtype, pairs, seq, V, logits, ldl, labels, mask, beta, smoothing);
+  if (rc != BAMBOO_OK) return rc;
+  if (!ref_logp || !lse || !logp || !logp_seq || !margin || !loss || !scratch || ((uintptr_t)scratch & 7)) return BAMBOO_E_ARG;
+  a.ref_logp = ref_logp; a.lse = lse; a.logp = logp; a.logp_seq = logp_seq; a.margin = margin; a.loss = loss; a.scratch = scratch;
+  (void)hipGetLastError();
+  return finish(launch_preference_fwd((hipStream_t)stream, dtype, a));
+}
+
+int bk_preference_loss_bwd(int dtype, int pairs, int seq, int V, const void* logits, int64_t ldl, const int32_t* labels,
+                           const uint8_t* mask, const float* lse, const float* margin, float beta, float smoothing,
+                           float scale, void* dlogits, int64_t ldd, void* stream) {
+  PreferenceDesc a;
+  const int rc = preference_desc(a, dtype, pairs, seq, V, logits, ldl, labels, mask, beta, smoothing);
+  if (rc != BAMBOO_OK) return rc;
+  if (!lse || !margin || !dlogits || bad_gradient(dtype, (int64_t)2 * pairs * seq, V, logits, ldl, dlogits, ldd)) return BAMBOO_E_ARG;
+  a.lse = (float*)lse; a.margin = (float*)margin; a.scale = scale; a.dlogits = dlogits; a.ldd = ldd;
+  (void)hipGetLastError();
+  return finish(launch_preference_bwd((hipStream_t)stream, dtype, a));
+}
+
+int bk_adamw_group(int dtype, int moment_bits, int n, const int64_t* numel, const float* const* g, float* const* master,
+                   void* const* m, void* const* v, float* const* m_scale, float* const* v_scale, void* const* w,
+                   const double* decay, double lr, double beta1, double beta2, double eps, int step, uint32_t seed,
+                   void* stream) {
+  if ((dtype != 0 && dtype != 1) || (moment_bits != 32 && moment_bits != 8) || n < 1 || step < 1) return BAMBOO_E_ARG;
+  if (!numel || !g || !master || !m || !v || !w || !decay || (moment_bits == 8) != (m_scale && v_scale)) return BAMBOO_E_ARG;
+  if ((moment_bits == 32 && (m_scale || v_scale)) || !(beta1 >= 0. && beta1 < 1.) || !(beta2 >= 0. && beta2 < 1.) || !(eps >= 0.))
+    return BAMBOO_E_ARG;
+  try {
+    std::vector<AdamwTensor> t((size_t)n);
+    std::vector<std::pair<uintptr_t, uintptr_t>> held;
+    held.reserve((size_t)n);
+    for (int i = 0; i < n; ++i) {
+      AdamwTensor& p = t[i];
+      memset(&p, 0, sizeof(p));
+      p.numel = numel[i];
+      if (p.numel < 0 || p.numel > (int64_t)1 << 40) return BAMBOO_E_ARG;
+      if (p.numel == 0) continue;
+      p.g = g[i]; p.master = master[i]; p.m = m[i]; p.v = v[i]; p.w = w[i];
+      if (!p.g || !p.master || !p.m || !p.v || !p.w || !element_aligned(dtype, p.w)) return BAMBOO_E_ARG;
+      uintptr_t words = (uintptr_t)p.g | (uintptr_t)p.master;
+      if (moment_bits == 8) {
+        p.m_scale = m_scale[i]; p.v_scale = v_scale[i];
+        if (!p.m_scale || !p.v_scale) return BAMBOO_E_ARG;
+        words |= (uintptr_t)p.m_scale | (uintptr_t)p.v_scale;
+      } else {
+        words |= (uintptr_t)p.m | (uintptr_t)p.v;
+      }
+      if (words & 3) return BAMBOO_E_ARG;
+      held.emplace_back((uintptr_t)p.master, (uintptr_t)(p.master + p.numel));
+    }
+    // the same weights twice would be two steps at once on one tensor
+    std::sort(held.begin(), held.end());
+    for (size_t i = 1; i < held.size(); ++i)
+      if (held[i].first < held[i - 1].second) return BAMBOO_E_ARG;
+    AdamwHyper h = {lr, beta1, beta2, eps, step};
+    (void)hipGetLastError();
+    return finish(launch_adamw((hipStream_t)stream, dtype, moment_bits, h, n, t.data(), decay, seed));
+  } catch (const std::bad_alloc&) {
+    return BAMBOO_E_NOMEM;
+  }
 }
 
 int bk_gemm_tile(int code) {
