@@ -608,53 +608,66 @@ def bk_ordered_sum(x, scale, out, stream=None):
 # cannot take as they are (another dtype or device than it needs, strides it does not know) are refused here, with the status
 # the library itself would give.
 
-def _refuse_unless(ok, where):
-    if not ok:
-        raise BambooError(E_ARG, where)
+# Checks go by plain numbers (a tensor's device as its index) and each property is asked for once: for a call of a few
+# microseconds on the device, this side is what its time is.
+
+_ACT = {torch.float32: 0, torch.bfloat16: 1}
+_get_device = torch.Tensor.get_device                       # index, -1 in host memory
+_current_device = torch._C._cuda_getDevice                  # as torch.cuda.current_device, behind its first use
+_raw_stream = torch._C._cuda_getCurrentRawStream            # address of a device's current stream
 
 
-def _rows(t, where, rows=None, cols=None, like=None):
-    """(address, row stride) of a matrix."""
-    _refuse_unless(t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and (rows is None or t.shape[0] == rows) and
-                   (cols is None or t.shape[1] == cols), where)
-    _refuse_unless(t.dtype in _ACT if like is None else t.dtype == like.dtype and t.device == like.device, where)
-    # the stride of a single row says nothing
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _refuse(where):
+    raise BambooError(E_ARG, where)
 
 
-def _vec(t, n, dtypes, like, where):
+def _rows(t, where, rows, cols, dtype, dev):
+    """(address, row stride) of a matrix of the given shape, dtype and device, whose columns are neighbours."""
+    st = t.stride()
+    if t.shape != (rows, cols) or (st[1] != 1 and cols > 1) or t.dtype != dtype or _get_device(t) != dev:
+        _refuse(where)
+    return t.data_ptr(), st[0] if rows > 1 else cols        # the stride of a single row says nothing
+
+
+def _vec(t, n, dtype, dev, where):
     """Address of n contiguous values, or None."""
     if t is None:
         return None
-    _refuse_unless(t.numel() == n and t.is_contiguous() and t.dtype in dtypes and t.device == like.device, where)
+    if t.numel() != n or t.dtype != dtype or _get_device(t) != dev or not t.is_contiguous():
+        _refuse(where)
     return t.data_ptr()
 
 
-_ACT = (torch.float32, torch.bfloat16)
-_F32, _I32, _U8 = (torch.float32,), (torch.int32,), (torch.uint8, torch.bool)
+def _mask(t, n, dev, where):
+    return _vec(t, n, torch.bool if t is not None and t.dtype == torch.bool else torch.uint8, dev, where)
 
 
-class _On:
-    """The tensor's device as the current one, and the address of the stream there (the current one if None is given)."""
-
-    def __init__(self, t, stream):
-        self.t, self.stream, self.guard = t, stream, None
-
-    def __enter__(self):
-        if self.t.device.type == "cuda" and self.t.device.index != torch.cuda.current_device():
-            self.guard = torch.cuda.device(self.t.device)
-            self.guard.__enter__()
-        return (self.stream if self.stream is not None else torch.cuda.current_stream()).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _first(t, where):
+    """(rows, columns, dtype, its code, device) of the matrix that the others go by."""
+    if t.dim() != 2 or t.dtype not in _ACT:
+        _refuse(where)
+    (rows, cols), dtype = t.shape, t.dtype
+    return rows, cols, dtype, _ACT[dtype], _get_device(t)
 
 
-def _scratch(n, like, stream):
+def _launch(fn, where, dev, stream, *args):
+    """fn(*args, stream) with `dev` as the current device, on its current stream if none is given."""
+    if dev < 0:
+        _refuse(where)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return _launch(fn, where, dev, stream, *args)
+    status = fn(*args, _raw_stream(dev) if stream is None else stream.cuda_stream)
+    if status < 0:
+        raise BambooError(status, where)
+
+
+def _scratch(n, dev, stream, where):
     """n floats of scratch for one call, held by the allocator until the call's stream is through with it."""
-    t = torch.empty(n, dtype=torch.float32, device=like.device)
-    if stream is not None and stream != torch.cuda.current_stream(like.device):
+    if dev < 0:
+        _refuse(where)
+    t = torch.empty(n, dtype=torch.float32, device=dev)
+    if stream is not None and stream.cuda_stream != _raw_stream(dev):
         t.record_stream(stream)
     return t
 
@@ -664,7 +677,8 @@ ROTARY_SCALINGS = ("none", "linear", "stretched", "parts")
 
 def bk_rotary_frequencies(rot, base=10000.0, scaling="none", factor=1.0, length=0, device="cuda:0"):
     """(frequencies of the rot/2 pairs as a float64 tensor on `device`, amplitude) for bk_rotary."""
-    _refuse_unless(scaling in ROTARY_SCALINGS and rot >= 2, "bk_rotary_frequencies")
+    if scaling not in ROTARY_SCALINGS or rot < 2:
+        _refuse("bk_rotary_frequencies")
     freq, amplitude = torch.empty(rot // 2, dtype=torch.float64), C.c_float()
     _check(lib.bk_rotary_frequencies(rot, base, ROTARY_SCALINGS.index(scaling), factor, length, freq.data_ptr(), C.byref(amplitude)),
            "bk_rotary_frequencies")
@@ -675,131 +689,132 @@ def bk_rotary(x, freq, y, heads, d, pos=None, seq=1, interleaved=False, inverse=
     """y = x with the first 2 * len(freq) features of its first `heads` heads turned by their positions (pos int32 [T], or
     t mod seq).  y may be x."""
     where = "bk_rotary"
-    px, ldx = _rows(x, where)
-    py, ldy = _rows(y, where, rows=x.shape[0], like=x)
-    _refuse_unless(min(x.shape[1], y.shape[1]) >= heads * d, where)
-    with _On(x, stream) as s:
-        _check(lib.bk_rotary(_dt(x), x.shape[0], seq, heads, d, 2 * freq.numel(), int(interleaved), int(inverse), px, ldx,
-                             _vec(pos, x.shape[0], _I32, x, where), _vec(freq, freq.numel(), (torch.float64,), x, where),
-                             amplitude, py, ldy, s), where)
+    T, cols, dtype, code, dev = _first(x, where)
+    px, ldx = _rows(x, where, T, cols, dtype, dev)
+    wide = y.shape[-1]
+    py, ldy = _rows(y, where, T, wide, dtype, dev)
+    if cols < heads * d or wide < heads * d:
+        _refuse(where)
+    half = freq.numel()
+    _launch(lib.bk_rotary, where, dev, stream, code, T, seq, heads, d, 2 * half, interleaved, inverse, px, ldx,
+            _vec(pos, T, torch.int32, dev, where), _vec(freq, half, torch.float64, dev, where), amplitude, py, ldy)
 
 
-def _cross_sizes(q, k, batch, heads, kv_heads, where):
-    _refuse_unless(batch > 0 and heads > 0 and kv_heads > 0 and q.dim() == 2 and k.dim() == 2 and q.shape[0] % batch == 0 and
-                   k.shape[0] % batch == 0 and q.shape[1] % heads == 0, where)
-    return q.shape[0] // batch, k.shape[0] // batch, q.shape[1] // heads
+def _cross(q, k, v, batch, heads, kv_heads, kv_len, where):
+    """Sizes, then the arguments that both directions share: (dtype, device, rows and columns of q, of k), sizes, addresses"""
+    rows, cols, dtype, code, dev = _first(q, where)
+    if batch <= 0 or heads <= 0 or kv_heads <= 0 or rows % batch or cols % heads or k.dim() != 2 or k.shape[0] % batch:
+        _refuse(where)
+    d, keys = cols // heads, k.shape[0]
+    pq, ldq = _rows(q, where, rows, cols, dtype, dev)
+    pk, ldk = _rows(k, where, keys, kv_heads * d, dtype, dev)
+    pv, ldv = _rows(v, where, keys, kv_heads * d, dtype, dev)
+    if ldk != ldv:
+        _refuse(where)
+    return ((where, rows, cols, dtype, dev), (where, keys, kv_heads * d, dtype, dev),
+            (batch, rows // batch, keys // batch, heads, kv_heads, d), code,
+            (pq, ldq, pk, pv, ldk, _vec(kv_len, batch, torch.int32, dev, where)))
 
 
 def bk_cross_attention_fwd(q, k, v, ctx, lse, batch, heads, kv_heads=None, kv_len=None, impl=0, stream=None):
     """ctx, lse of q [batch*sq, heads*d] over k, v [batch*sk, kv_heads*d]; kv_len: int32 [batch].  Returns the call's scratch."""
     where = "bk_cross_attention_fwd"
-    kv_heads = heads if kv_heads is None else kv_heads
-    sq, sk, d = _cross_sizes(q, k, batch, heads, kv_heads, where)
-    pq, ldq = _rows(q, where)
-    pk, ldk = _rows(k, where, cols=kv_heads * d, like=q)
-    pv, ldv = _rows(v, where, rows=k.shape[0], cols=kv_heads * d, like=q)
-    pc, ldc = _rows(ctx, where, rows=q.shape[0], cols=q.shape[1], like=q)
-    _refuse_unless(ldk == ldv, where)
-    with _On(q, stream) as s:
-        scratch = _scratch(lib.bk_cross_attention_scratch_floats(batch, sq, sk, heads, kv_heads, d), q, stream)
-        _check(lib.bk_cross_attention_fwd(_dt(q), impl, batch, sq, sk, heads, kv_heads, d, pq, ldq, pk, pv, ldk,
-                                          _vec(kv_len, batch, _I32, q, where), pc, ldc,
-                                          _vec(lse, batch * heads * sq, _F32, q, where), scratch.data_ptr(), s), where)
+    like_q, _, sizes, code, inputs = _cross(q, k, v, batch, heads, heads if kv_heads is None else kv_heads, kv_len, where)
+    rows, dev = like_q[1], like_q[4]
+    n = lib.bk_cross_attention_scratch_floats(*sizes)
+    scratch = _scratch(n, dev, stream, where) if n else None
+    _launch(lib.bk_cross_attention_fwd, where, dev, stream, code, impl, *sizes, *inputs, *_rows(ctx, *like_q),
+            _vec(lse, rows * heads, torch.float32, dev, where), scratch.data_ptr() if n else None)
     return scratch
 
 
 def bk_cross_attention_bwd(q, k, v, ctx, lse, dctx, dq, dk, dv, batch, heads, kv_heads=None, kv_len=None, impl=0, stream=None):
     """dq, dk, dv from dctx, with ctx and lse of the forward.  Returns the call's scratch."""
     where = "bk_cross_attention_bwd"
-    kv_heads = heads if kv_heads is None else kv_heads
-    sq, sk, d = _cross_sizes(q, k, batch, heads, kv_heads, where)
-    pq, ldq = _rows(q, where)
-    (pc, ldc), (pg, ldg), (pdq, lddq) = (_rows(t, where, q.shape[0], q.shape[1], q) for t in (ctx, dctx, dq))
-    (pk, ldk), (pv, ldv), (pdk, lddk), (pdv, lddv) = (_rows(t, where, k.shape[0], kv_heads * d, q) for t in (k, v, dk, dv))
-    _refuse_unless(ldk == ldv and lddk == lddv, where)
-    with _On(q, stream) as s:
-        scratch = _scratch(lib.bk_cross_attention_scratch_floats(batch, sq, sk, heads, kv_heads, d), q, stream)
-        _check(lib.bk_cross_attention_bwd(_dt(q), impl, batch, sq, sk, heads, kv_heads, d, pq, ldq, pk, pv, ldk,
-                                          _vec(kv_len, batch, _I32, q, where), pc, ldc,
-                                          _vec(lse, batch * heads * sq, _F32, q, where), pg, ldg, pdq, lddq, pdk, pdv, lddk,
-                                          scratch.data_ptr(), s), where)
+    like_q, like_k, sizes, code, inputs = _cross(q, k, v, batch, heads, heads if kv_heads is None else kv_heads, kv_len, where)
+    rows, dev = like_q[1], like_q[4]
+    (pdk, lddk), (pdv, lddv) = _rows(dk, *like_k), _rows(dv, *like_k)
+    if lddk != lddv:
+        _refuse(where)
+    scratch = _scratch(lib.bk_cross_attention_scratch_floats(*sizes), dev, stream, where)
+    _launch(lib.bk_cross_attention_bwd, where, dev, stream, code, impl, *sizes, *inputs, *_rows(ctx, *like_q),
+            _vec(lse, rows * heads, torch.float32, dev, where), *_rows(dctx, *like_q), *_rows(dq, *like_q), pdk, pdv, lddk,
+            scratch.data_ptr())
     return scratch
 
 
 def bk_policy_loss(logits, labels, old_logp, adv, logp, loss_tok, dlogits=None, mask=None, ref_logp=None, kl_tok=None,
                    entropy=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0, ent_coef=0.0, scale=1.0, stream=None):
     """Per token: clipped policy loss with a KL and an entropy term, and (dlogits) scale times its gradient."""
-    where = "bk_policy_loss"
-    pl, ldl = _rows(logits, where)
-    T, V = logits.shape
-    pd, ldd = (None, 0) if dlogits is None else _rows(dlogits, where, T, V, logits)
-    f = [_vec(t, T, _F32, logits, where) for t in (old_logp, ref_logp, adv, logp, loss_tok, kl_tok, entropy)]
-    with _On(logits, stream) as s:
-        _check(lib.bk_policy_loss(_dt(logits), T, V, pl, ldl, _vec(labels, T, _I32, logits, where), _vec(mask, T, _U8, logits, where),
-                                  f[0], f[1], f[2], clip_low, clip_high, kl_coef, ent_coef, scale, f[3], f[4], f[5], f[6], pd, ldd,
-                                  s), where)
+    where, f32 = "bk_policy_loss", torch.float32
+    T, V, dtype, code, dev = _first(logits, where)
+    pl, ldl = _rows(logits, where, T, V, dtype, dev)
+    pd, ldd = (None, 0) if dlogits is None else _rows(dlogits, where, T, V, dtype, dev)
+    _launch(lib.bk_policy_loss, where, dev, stream, code, T, V, pl, ldl, _vec(labels, T, torch.int32, dev, where),
+            _mask(mask, T, dev, where), _vec(old_logp, T, f32, dev, where), _vec(ref_logp, T, f32, dev, where),
+            _vec(adv, T, f32, dev, where), clip_low, clip_high, kl_coef, ent_coef, scale, _vec(logp, T, f32, dev, where),
+            _vec(loss_tok, T, f32, dev, where), _vec(kl_tok, T, f32, dev, where), _vec(entropy, T, f32, dev, where), pd, ldd)
 
 
 def bk_preference_loss_fwd(logits, labels, ref_logp, lse, logp, logp_seq, margin, loss, beta, smoothing=0.0, mask=None, stream=None):
     """Per pair: margin and loss; logits of the chosen sequences, then of the rejected ones.  Returns the call's scratch."""
-    where = "bk_preference_loss_fwd"
-    pl, ldl = _rows(logits, where)
-    (T, V), pairs = logits.shape, loss.numel()
-    _refuse_unless(pairs > 0 and T % (2 * pairs) == 0, where)
-    vec = lambda t, n: _vec(t, n, _F32, logits, where)
-    with _On(logits, stream) as s:
-        scratch = _scratch(2 * T, logits, stream)
-        _check(lib.bk_preference_loss_fwd(_dt(logits), pairs, T // (2 * pairs), V, pl, ldl, _vec(labels, T, _I32, logits, where),
-                                          _vec(mask, T, _U8, logits, where), vec(ref_logp, 2 * pairs), beta, smoothing, vec(lse, T),
-                                          vec(logp, T), vec(logp_seq, 2 * pairs), vec(margin, pairs), vec(loss, pairs),
-                                          scratch.data_ptr(), s), where)
+    where, f32 = "bk_preference_loss_fwd", torch.float32
+    T, V, dtype, code, dev = _first(logits, where)
+    n = loss.numel()
+    if n == 0 or T % (2 * n):
+        _refuse(where)
+    pl, ldl = _rows(logits, where, T, V, dtype, dev)
+    scratch = _scratch(2 * T, dev, stream, where)
+    _launch(lib.bk_preference_loss_fwd, where, dev, stream, code, n, T // (2 * n), V, pl, ldl,
+            _vec(labels, T, torch.int32, dev, where), _mask(mask, T, dev, where), _vec(ref_logp, 2 * n, f32, dev, where), beta,
+            smoothing, _vec(lse, T, f32, dev, where), _vec(logp, T, f32, dev, where), _vec(logp_seq, 2 * n, f32, dev, where),
+            _vec(margin, n, f32, dev, where), _vec(loss, n, f32, dev, where), scratch.data_ptr())
     return scratch
 
 
 def bk_preference_loss_bwd(logits, labels, lse, margin, dlogits, beta, smoothing=0.0, scale=1.0, mask=None, stream=None):
     """dlogits = scale times the gradient of the pairs' losses."""
     where = "bk_preference_loss_bwd"
-    pl, ldl = _rows(logits, where)
-    (T, V), pairs = logits.shape, margin.numel()
-    _refuse_unless(pairs > 0 and T % (2 * pairs) == 0, where)
-    pd, ldd = _rows(dlogits, where, T, V, logits)
-    with _On(logits, stream) as s:
-        _check(lib.bk_preference_loss_bwd(_dt(logits), pairs, T // (2 * pairs), V, pl, ldl, _vec(labels, T, _I32, logits, where),
-                                          _vec(mask, T, _U8, logits, where), _vec(lse, T, _F32, logits, where),
-                                          _vec(margin, pairs, _F32, logits, where), beta, smoothing, scale, pd, ldd, s), where)
+    T, V, dtype, code, dev = _first(logits, where)
+    n = margin.numel()
+    if n == 0 or T % (2 * n):
+        _refuse(where)
+    pl, ldl = _rows(logits, where, T, V, dtype, dev)
+    pd, ldd = _rows(dlogits, where, T, V, dtype, dev)
+    _launch(lib.bk_preference_loss_bwd, where, dev, stream, code, n, T // (2 * n), V, pl, ldl,
+            _vec(labels, T, torch.int32, dev, where), _mask(mask, T, dev, where), _vec(lse, T, torch.float32, dev, where),
+            _vec(margin, n, torch.float32, dev, where), beta, smoothing, scale, pd, ldd)
+
+
+_CODES = (torch.uint8, torch.float8_e4m3fn)
 
 
 def bk_adamw_group(gs, masters, ms, vs, ws, step, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, decay=0.0, m_scales=None,
                    v_scales=None, seed=0, stream=None):
     """One AdamW step over lists of tensors: fp32 gradients and master weights, moments (fp32, or one-byte codes with fp32
     scales per 256 elements), storage weights.  decay: a number, or one per tensor."""
-    where, n = "bk_adamw_group", len(masters)
-    eight = m_scales is not None
-    _refuse_unless(n > 0 and len(ws) == n, where)
-    moments = _CODES if eight else _F32
-    lists = [(gs, _F32), (masters, _F32), (ms, moments), (vs, moments), (ws, (ws[0].dtype,))]
+    where, n, eight = "bk_adamw_group", len(masters), m_scales is not None
+    if n == 0 or len(ws) != n or ws[0].dtype not in _ACT or (v_scales is not None) != eight:
+        _refuse(where)
+    decay = [decay] * n if isinstance(decay, (int, float)) else decay
+    f32, act, dev, moments = torch.float32, ws[0].dtype, _get_device(masters[0]), _CODES if eight else (torch.float32,)
     numel = [t.numel() for t in masters]
-    _refuse_unless(ws[0].dtype in _ACT and (v_scales is not None) == eight, where)
-    decay = [decay] * n if isinstance(decay, (int, float)) else list(decay)
-    _refuse_unless(len(decay) == n, where)
-    device, ptrs = masters[0].device, []
-    for ts, dtypes in lists:
-        _refuse_unless(len(ts) == n, where)
-        for t, k in zip(ts, numel):
-            _refuse_unless(t.numel() == k and t.dtype in dtypes and t.is_contiguous() and t.device == device, where)
-        ptrs.append((_vp * n)(*[t.data_ptr() for t in ts]))
-    for ts in (m_scales, v_scales):
-        if eight:
-            _refuse_unless(len(ts) == n, where)
-            for t, k in zip(ts, numel):
-                _refuse_unless(t.numel() == -(-k // 256) and t.dtype in _F32 and t.is_contiguous() and t.device == device, where)
-        ptrs.append((_vp * n)(*[t.data_ptr() for t in ts]) if eight else None)
-    with _On(masters[0], stream) as s:
-        _check(lib.bk_adamw_group(_dt(ws[0]), 8 if eight else 32, n, (C.c_int64 * n)(*numel), ptrs[0], ptrs[1], ptrs[2], ptrs[3],
-                                  ptrs[5], ptrs[6], ptrs[4], (C.c_double * n)(*decay), lr, beta1, beta2, eps, step, seed & 0xFFFFFFFF, s), where)
+    scales = [-(-k // 256) for k in numel] if eight else None
 
-
-_CODES = (torch.uint8, torch.float8_e4m3fn)
+    def addresses(ts, sizes, dtypes):
+        if len(ts) != n:
+            _refuse(where)
+        for t, k in zip(ts, sizes):
+            if t.numel() != k or t.dtype not in dtypes or _get_device(t) != dev or not t.is_contiguous():
+                _refuse(where)
+        return (_vp * n)(*[t.data_ptr() for t in ts])
+    if len(decay) != n:
+        _refuse(where)
+    pg, pw = addresses(gs, numel, (f32,)), addresses(masters, numel, (f32,))
+    pm, pv, out = addresses(ms, numel, moments), addresses(vs, numel, moments), addresses(ws, numel, (act,))
+    sm, sv = (addresses(m_scales, scales, (f32,)), addresses(v_scales, scales, (f32,))) if eight else (None, None)
+    _launch(lib.bk_adamw_group, where, dev, stream, _ACT[act], 8 if eight else 32, n, (C.c_int64 * n)(*numel), pg, pw, pm, pv, sm, sv,
+            out, (C.c_double * n)(*decay), lr, beta1, beta2, eps, step, seed & 0xFFFFFFFF)
 
 
 def bk_gemm_stages(n):

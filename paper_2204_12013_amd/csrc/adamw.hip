@@ -93,11 +93,6 @@ __device__ __forceinline__ f32x4 decode(unsigned c, float scale) {
   v[3] = __builtin_amdgcn_cvt_f32_fp8((int)c, 3) * scale;
   return v;
 }
-__device__ __forceinline__ unsigned encode(const f32x4& q) {            // of values that have a code
-  int c = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
-  return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], c, true);
-}
-
 __host__ __device__ __forceinline__ unsigned mix(unsigned x) {
   x ^= x >> 16;
   x *= 0x7feb352du;
@@ -106,14 +101,15 @@ __host__ __device__ __forceinline__ unsigned mix(unsigned x) {
   return x ^ (x >> 16);
 }
 
-// |x| inv, at most 448, moved to one of the two codes around it: up where the part beyond the lower one and `up` make a
-// whole step.  Codes are 2^(e-3) apart in [2^e, 2^(e+1)), and 2^-9 below 2^-6.
-__device__ __forceinline__ float to_code(float x, float inv, unsigned up16) {
-  const float q = fminf(fabsf(x) * inv, 448.f);
-  const unsigned e = max(__builtin_bit_cast(unsigned, q) >> 23, 121u) - 3u;       // biased exponent of the step
-  const float step = __builtin_bit_cast(float, e << 23), per = __builtin_bit_cast(float, (254u - e) << 23);
-  const float n = floorf(fmaf(q, per, ((float)up16 + 0.5f) * (1.f / 65536.f)));
-  return x == x ? fminf(n * step, 448.f) : x;
+// |x| inv, at most 448, moved to one of the two codes around it: up where the part beyond the lower one and `up` / 65536 (plus
+// half of that unit) make a whole step, codes being 2^(e-3) apart in [2^e, 2^(e+1)) and 2^-9 below 2^-6.  The conversion
+// adds 20 bits behind the code's last, of which these are the first 17; NaN stays NaN.
+__device__ __forceinline__ float scaled(float x, float inv) {
+  const float q = x * inv;
+  return x == x ? fminf(fmaxf(q, -448.f), 448.f) : x;
+}
+template <int J> __device__ __forceinline__ int put_code(float q, unsigned up, int c) {
+  return __builtin_amdgcn_cvt_sr_fp8_f32(q, (int)(up << 16 | 0x8000u), c, J);
 }
 
 template <typename T, int BITS, bool STREAM>
@@ -149,11 +145,13 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwBatch a) {
   for (int u = 0; u < kGroups; ++u) {
     const long at = start + u * 256;
     if (left[u] <= 0) continue;
+    f32x4 root;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       m[u][j] = a.beta1 * m[u][j] + a.not_beta1 * g[u][j];
       v[u][j] = a.beta2 * v[u][j] + a.not_beta2 * g[u][j] * g[u][j];
-      w[u][j] = w[u][j] * p.keep - a.lr * (m[u][j] * a.inv_c1) / (sqrtf(v[u][j] * a.inv_c2) + a.eps);
+      root[j] = sqrtf(v[u][j]);
+      w[u][j] = w[u][j] * p.keep - a.lr_c1 * m[u][j] / fmaf(root[j], a.root_c2, a.eps);
     }
     put4<STREAM>(p.master + at, w[u], vec[u], lane, left[u]);
     put_storage((T*)p.w + at, w[u], vec[u], lane, left[u]);            // read by the next iteration
@@ -165,28 +163,34 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwBatch a) {
     float top_m = 0.f, top_v = 0.f;                                    // elements behind the end are 0
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      v[u][j] = sqrtf(v[u][j]);
       top_m = fmaxf(top_m, fabsf(m[u][j]));
-      top_v = fmaxf(top_v, v[u][j]);
+      top_v = fmaxf(top_v, root[j]);
     }
     top_m = wave_max(top_m);
     top_v = wave_max(top_v);
     // a block with nothing above 1e-30 becomes zeros: 448 / top would leave the range
     const float inv_m = top_m > 1e-30f ? 448.f / top_m : 0.f, inv_v = top_v > 1e-30f ? 448.f / top_v : 0.f;
-    f32x4 cm, cv;
+    unsigned h[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const unsigned i = (unsigned)at + (vec[u] ? 4 * lane + j : 64 * j + lane);
-      const unsigned h = mix(i ^ p.key);
-      cm[j] = copysignf(to_code(m[u][j], inv_m, h & 0xffffu), m[u][j]);
-      cv[j] = to_code(v[u][j], inv_v, h >> 16);
-      if (v[u][j] > 0.f) cv[j] = fmaxf(cv[j], 0.001953125f);           // the smallest code
+      h[j] = mix(i ^ p.key);
+      m[u][j] = scaled(m[u][j], inv_m);
+      root[j] = scaled(root[j], inv_v);
     }
-    put_codes((unsigned char*)p.m + at, encode(cm), vec[u], lane, left[u]);
-    put_codes((unsigned char*)p.v + at, encode(cv), vec[u], lane, left[u]);
+    int cm = put_code<0>(m[u][0], h[0], 0), cv = put_code<0>(root[0], h[0] >> 16, 0);
+    cm = put_code<1>(m[u][1], h[1], cm), cv = put_code<1>(root[1], h[1] >> 16, cv);
+    cm = put_code<2>(m[u][2], h[2], cm), cv = put_code<2>(root[2], h[2] >> 16, cv);
+    cm = put_code<3>(m[u][3], h[3], cm), cv = put_code<3>(root[3], h[3] >> 16, cv);
+    // a root that is not zero has the smallest code at least; it is a code's last bit
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (v[u][j] > 0.f && ((unsigned)cv >> (8 * j) & 0xffu) == 0) cv |= 1 << (8 * j);
+    put_codes((unsigned char*)p.m + at, (unsigned)cm, vec[u], lane, left[u]);
+    put_codes((unsigned char*)p.v + at, (unsigned)cv, vec[u], lane, left[u]);
     if (lane == 0) {
-      p.m_scale[at >> 8] = top_m / 448.f;
-      p.v_scale[at >> 8] = top_v / 448.f;
+      p.m_scale[at >> 8] = top_m * (1.f / 448.f);
+      p.v_scale[at >> 8] = top_v * (1.f / 448.f);
     }
   }
 }
@@ -203,14 +207,13 @@ hipError_t adamw_launch(hipStream_t s, const AdamwBatch& b, int wgs, bool stream
 hipError_t launch_adamw(hipStream_t s, int dtype, int bits, const AdamwHyper& h, int n, const AdamwTensor* t, const double* decay,
                         uint32_t seed) {
   AdamwBatch b;
-  b.lr = (float)h.lr;
   b.beta1 = (float)h.beta1;
   b.beta2 = (float)h.beta2;
   b.not_beta1 = (float)(1. - h.beta1);
   b.not_beta2 = (float)(1. - h.beta2);
   b.eps = (float)h.eps;
-  b.inv_c1 = (float)(1. / (1. - pow(h.beta1, (double)h.step)));
-  b.inv_c2 = (float)(1. / (1. - pow(h.beta2, (double)h.step)));
+  b.lr_c1 = (float)(h.lr / (1. - pow(h.beta1, (double)h.step)));
+  b.root_c2 = (float)sqrt(1. / (1. - pow(h.beta2, (double)h.step)));
   long total = 0;
   for (int i = 0; i < n; ++i) total += t[i].numel;
   const bool stream = streams_past_cache(total * ((bits == 32 ? 28 : 16) + (dtype == 1 ? 2 : 4)));

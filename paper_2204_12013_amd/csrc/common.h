@@ -386,7 +386,7 @@ struct AdamwTensor {
 struct AdamwBatch {
   AdamwTensor t[kAdamwTensors];
   int n;
-  float lr, beta1, beta2, not_beta1, not_beta2, eps, inv_c1, inv_c2;
+  float beta1, beta2, not_beta1, not_beta2, eps, lr_c1, root_c2;   // lr / (1 - beta1^step), 1 / sqrt(1 - beta2^step)
 };
 static_assert(sizeof(AdamwBatch) <= 4096 - 256, "kernel arguments, with room for the hidden ones");
 struct AdamwHyper {

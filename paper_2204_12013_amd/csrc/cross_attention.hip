@@ -9,6 +9,7 @@ namespace bamboo {
 namespace {
 
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kNone = -1.0e30f;     // maximum of no scores
 
 // Row of `rows` per pair: out = sum of the parts, weighted to their common maximum.  One wavefront a row.
 template <typename T>
@@ -18,19 +19,41 @@ __global__ __launch_bounds__(256) void cross_join_fwd_kernel(CrossDesc a) {
   if (i >= n) return;
   const int pair = (int)(i / a.rows), b = pair / a.kv_heads;
   const CrossRow at = cross_row(a, pair % a.kv_heads, (int)(i % a.rows));
-  float m = -INFINITY;
-  for (int s = 0; s < a.splits; ++s)
-    if (a.part_stats[2 * (s * n + i) + 1] != 0.f) m = fmaxf(m, a.part_stats[2 * (s * n + i)]);     // parts that had keys
-  float l = 0.f, o0 = 0.f, o1 = 0.f;
-  for (int s = 0; s < a.splits; ++s) {
-    const long p = s * n + i;
-    const float ls = a.part_stats[2 * p + 1];
-    if (ls == 0.f) continue;
-    const float w = __builtin_amdgcn_exp2f(a.part_stats[2 * p] - m);
-    l = fmaf(w, ls, l);
-    if (lane < a.d) o0 = fmaf(w, a.part[p * a.d + lane], o0);
-    if (lane + 64 < a.d) o1 = fmaf(w, a.part[p * a.d + lane + 64], o1);
+  // 64 parts at a time, one a lane: their maxima and sums, then their weights; the rows of eight parts are requested together
+  float m = kNone, l = 0.f, o0 = 0.f, o1 = 0.f;
+  const int c0 = min(lane, a.d - 1), c1 = min(lane + 64, a.d - 1);
+  for (int s0 = 0; s0 < a.splits; s0 += 64) {
+    const int k = min(64, a.splits - s0);
+    const long p = (long)(s0 + min(lane, k - 1)) * n + i;
+    float ms = a.part_stats[2 * p], ls = a.part_stats[2 * p + 1];
+    if (lane >= k || ls == 0.f) {                 // no part, or one without keys
+      ms = kNone;
+      ls = 0.f;
+    }
+    const float to = fmaxf(m, wave_max(ms)), old = __builtin_amdgcn_exp2f(m - to);
+    const float w = ls == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms - to);
+    l = l * old + wave_sum_of_products(w, ls);
+    o0 *= old;
+    o1 *= old;
+    m = to;
+    const float* row = a.part + ((long)s0 * n + i) * a.d;
+    for (int s = 0; s < k; s += 8) {
+      float x0[8], x1[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const float* at_row = row + (long)min(s + q, k - 1) * n * a.d;
+        x0[q] = at_row[c0];
+        x1[q] = at_row[c1];
+      }
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const float wq = s + q < k ? of_lane(w, min(s + q, k - 1)) : 0.f;
+        o0 = wq > 0.f ? fmaf(wq, x0[q], o0) : o0;
+        o1 = wq > 0.f ? fmaf(wq, x1[q], o1) : o1;
+      }
+    }
   }
+  l = of_lane(l, 0);
   const float inv = l > 0.f ? 1.f / l : l;
   T* out = (T*)a.ctx + ((long)b * a.sq + at.query) * a.ldc + (long)at.head * a.d;
   if (lane < a.d) out[lane] = from_f32<T>(o0 * inv);
@@ -72,7 +95,7 @@ hipError_t join_bwd(hipStream_t s, int dtype, const CrossDesc& a) {
 // every CU a workgroup, otherwise as many as make two workgroups a CU, of four tiles at least.
 int parts(long owned, long streamed, long pairs) {
   const long wgs = (owned + 127) / 128 * pairs, tiles = (streamed + 63) / 64;
-  if (wgs >= 256 || tiles < 8) return 1;
+  if (wgs >= 512 || tiles < 8 || (wgs >= 256 && tiles < 64)) return 1;
   long n = (512 + wgs - 1) / wgs;
   if (n > tiles / 4) n = tiles / 4;
   return (int)(n < 1 ? 1 : n);

@@ -260,9 +260,13 @@ __global__ __launch_bounds__(256, 2) void cross_dq_mfma_kernel(CrossDesc a) {
     delta += other_half(delta);
   }
   if (lane < 32 && live && w.split == 0) a.delta[stat] = delta;
-  f32x16 neg_delta;                               // the dP products start from -delta
+  f32x16 neg_delta, neg_lse;                      // the products start from these: dP less delta, scores less the log-sum-exp
+  const float lse_s = -a.lse[stat] * sqrtf((float)D);
 #pragma unroll
-  for (int r = 0; r < 16; ++r) neg_delta[r] = -delta;
+  for (int r = 0; r < 16; ++r) {
+    neg_delta[r] = -delta;
+    neg_lse[r] = lse_s;
+  }
   wait_tiles<0>();
   __syncthreads();
   for (int t = 0; t < nt; ++t) {
@@ -274,35 +278,27 @@ __global__ __launch_bounds__(256, 2) void cross_dq_mfma_kernel(CrossDesc a) {
       copy.issue(vb, t0 + t + 1, ring + (slot ^ 1) * 2 * TB + TB);
     }
     if (busy) {
-      f32x16 s[2], dp[2];
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
+      for (int u = 0; u < 2; ++u) {
+        f32x16 s, dp;
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_k(buf, 0, u * 32, ks), qf[ks], ks == 0 ? zero16 : s[u], 0, 0, 0);
-          dp[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_k(buf, TB, u * 32, ks), dof[ks], ks == 0 ? neg_delta : dp[u], 0,
-                                                          0, 0);
+        for (int ks = 0; ks < D / 16; ++ks) {
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_k(buf, 0, u * 32, ks), qf[ks], ks == 0 ? neg_lse : s, 0, 0, 0);
+          dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_k(buf, TB, u * 32, ks), dof[ks], ks == 0 ? neg_delta : dp, 0, 0, 0);
         }
-      if (k0 + TILE > len) {
+        if (k0 + u * 32 + 32 > len) {               // the last keys
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+          for (int r = 0; r < 16; ++r) s[r] = k0 + u * 32 + acc_row(r) < len ? s[r] : kMasked;
+        }
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -lse2));
-            s[u][r] = k0 + u * 32 + acc_row(r) < len ? p * dp[u][r] : 0.f;       // dS^T
-          }
-      } else {
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] * c) * dp[r];       // dS^T
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int h = 0; h < 2; ++h) {
+          const bf16x8 dsb = pack8(s, h);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[u][r] = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -lse2)) * dp[u][r];
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const bf16x8 dsb = pack8(s[u >> 1], u & 1);
-#pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt)
-          dq[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_tr(buf, 0, dt, 16 * u), dsb, dq[dt], 0, 0, 0);
+          for (int dt = 0; dt < D / 32; ++dt)
+            dq[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_tr(buf, 0, dt, 32 * u + 16 * h), dsb, dq[dt], 0, 0, 0);
+        }
       }
     }
     wait_tiles<0>();
@@ -322,15 +318,12 @@ __global__ __launch_bounds__(256, 2) void cross_dq_mfma_kernel(CrossDesc a) {
 // Rows of the pair, 64 to a tile, from wherever their query and head are.  Offsets in 32 bits: see covers().
 template <int D>
 struct RowCopy {
-  static constexpr int N = TileCopy<D>::N;
-  unsigned col[N];
-  unsigned wave_lds;
+  static constexpr int N = TileCopy<D>::N, STEP = 256 / (D / 8);     // rows between a thread's chunks: their places are alike
+  static_assert(STEP % 16 == 0, "swz repeats after 16 rows");
+  unsigned col, wave_lds;
   __device__ __forceinline__ void init() {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int c = threadIdx.x + i * 256, r = c / (D / 8);
-      col[i] = (unsigned)(((c % (D / 8)) ^ swz<D>(r)) * 8) * 2u;
-    }
+    const int r = threadIdx.x / (D / 8);
+    col = (unsigned)(((threadIdx.x % (D / 8)) ^ swz<D>(r)) * 8) * 2u;
     wave_lds = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 1024;
   }
   // the same rows of two tensors
@@ -338,9 +331,9 @@ struct RowCopy {
                                         unsigned lds1, int tile) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int r = min(tile * TILE + (int)(threadIdx.x + i * 256) / (D / 8), a.rows - 1);
+      const int r = min(tile * TILE + (int)threadIdx.x / (D / 8) + i * STEP, a.rows - 1);
       const CrossRow p = cross_row(a, 0, r);
-      const unsigned in_row = (unsigned)p.head * (D * 2) + col[i];
+      const unsigned in_row = (unsigned)p.head * (D * 2) + col;
       asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                    :
                    : "v"((unsigned)p.query * (unsigned)(ld0 * 2) + in_row), "s"(g0), "s"(lds0 + wave_lds + i * 4096)
@@ -355,11 +348,11 @@ struct RowCopy {
 
 // Owns keys, streams rows.
 template <int D>
-__global__ __launch_bounds__(256, D == 64 ? 2 : 1) void cross_dkv_mfma_kernel(CrossDesc a) {
+__global__ __launch_bounds__(256, 2) void cross_dkv_mfma_kernel(CrossDesc a) {
   constexpr unsigned TB = TileCopy<D>::BYTES;
   extern __shared__ __attribute__((aligned(256))) unsigned char smem_raw[];
   const unsigned ring = lds_address(smem_raw);    // [2][queries, gradients]
-  float* lse_s = (float*)(smem_raw + 4 * TB);     // [2][64] (log2 domain), behind the tiles
+  float* lse_s = (float*)(smem_raw + 4 * TB);     // [2][64], behind the tiles
   float* del_s = lse_s + 2 * TILE;                // [2][64]
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 5;
   const CrossBlock w = cross_block(a);
@@ -371,12 +364,13 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void cross_dkv_mfma_kernel(Cr
   const bool busy = kw0 < len;
   const bf16_t* qb = (const bf16_t*)a.q + (long)w.b * a.sq * a.ldq + w.kvh * a.group * D;
   const bf16_t* gb = (const bf16_t*)a.dctx + (long)w.b * a.sq * a.lddc + w.kvh * a.group * D;
-  const float scale = rsqrtf((float)D), c = scale * kLog2e;
+  const float scale = rsqrtf((float)D), rscale = sqrtf((float)D), c = scale * kLog2e;
 
   bf16x8 kf[D / 16], vf[D / 16];
   const long at_key = ((long)w.b * a.sk + min(key, a.sk - 1)) * a.ldkv + w.kvh * D;
   lane_row<D>(kf, (const bf16_t*)a.k + at_key, key < len);
   lane_row<D>(vf, (const bf16_t*)a.v + at_key, key < len);
+  const float shut = key < len ? 0.f : kMasked;   // keys that do not count: exponents of their probabilities
   f32x16 dk[D / 32], dv[D / 32];
   clear(dk);
   clear(dv);
@@ -385,8 +379,9 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void cross_dkv_mfma_kernel(Cr
     if (threadIdx.x < TILE) {
       const int r = r0 + threadIdx.x;
       const long stat = cross_stat(a, w.b, cross_row(a, w.kvh, min(r, a.rows - 1)));
-      lse_r = a.lse[stat] * kLog2e;
-      del_r = -a.delta[stat];                     // negated: the dP accumulators start from it
+      // the accumulators start from these: scores come out less the log-sum-exp, dP less delta
+      lse_r = r < a.rows ? -a.lse[stat] * rscale : kMasked;    // behind the last row: probabilities of 0
+      del_r = -a.delta[stat];
     }
   };
   auto stash_stats = [&](int buf) {
@@ -409,69 +404,54 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void cross_dkv_mfma_kernel(Cr
   for (int t = 0; t < nt; ++t) {
     const int slot = t & 1;
     const unsigned buf = ring + slot * 2 * TB;
-    const int r0 = (t0 + t) * TILE;
     if (t + 1 < nt) {
-      fetch_stats(r0 + TILE);
+      fetch_stats((t0 + t + 1) * TILE);
       copy.issue(a, qb, a.ldq, ring + (slot ^ 1) * 2 * TB, gb, a.lddc, ring + (slot ^ 1) * 2 * TB + TB, t0 + t + 1);
     }
     if (busy) {
-      f32x16 s[2], dp[2];
+      // 32 rows at a time: the second half's scores would be 32 registers more
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < 2; ++u) {
+        f32x16 s, dp;
 #pragma unroll
         for (int a4 = 0; a4 < 4; ++a4) {
+          const f32x4 l4 = *(const f32x4*)(lse_s + slot * TILE + u * 32 + 8 * a4 + 4 * g);
           const f32x4 d4 = *(const f32x4*)(del_s + slot * TILE + u * 32 + 8 * a4 + 4 * g);
 #pragma unroll
-          for (int cc = 0; cc < 4; ++cc) dp[u][4 * a4 + cc] = d4[cc];
-        }
-      const f32x16 zero16 = {};
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          s[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_k(buf, 0, u * 32, ks), kf[ks], ks == 0 ? zero16 : s[u], 0, 0, 0);
-          dp[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_k(buf, TB, u * 32, ks), vf[ks], dp[u], 0, 0, 0);
-        }
-      const bool need_mask = (r0 + TILE > a.rows) || (kw0 + 32 > len);
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int a4 = 0; a4 < 4; ++a4) {
-          const int first = u * 32 + 8 * a4 + 4 * g;   // of 4 consecutive rows of this lane
-          const f32x4 l4 = *(const f32x4*)(lse_s + slot * TILE + first);
-          if (need_mask) {                             // uniform over the wavefront
-#pragma unroll
-            for (int cc = 0; cc < 4; ++cc) {
-              const int r = 4 * a4 + cc;
-              const bool counts = r0 + first + cc < a.rows && key < len;
-              const float p = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -l4[cc]));
-              s[u][r] = counts ? p : 0.f;
-              dp[u][r] = counts ? dp[u][r] * p : 0.f;  // dS
-            }
-          } else {
-#pragma unroll
-            for (int cc = 0; cc < 4; ++cc) {
-              const int r = 4 * a4 + cc;
-              const float p = __builtin_amdgcn_exp2f(fmaf(s[u][r], c, -l4[cc]));
-              s[u][r] = p;
-              dp[u][r] *= p;
-            }
+          for (int cc = 0; cc < 4; ++cc) {
+            s[4 * a4 + cc] = l4[cc];
+            dp[4 * a4 + cc] = d4[cc];
           }
         }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const bf16x8 pb = pack8(s[u >> 1], u & 1);
-        const bf16x8 dsb = pack8(dp[u >> 1], u & 1);
-#pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt) {
-          dv[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_tr(buf, TB, dt, 16 * u), pb, dv[dt], 0, 0, 0);
-          dk[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_tr(buf, 0, dt, 16 * u), dsb, dk[dt], 0, 0, 0);
+        for (int ks = 0; ks < D / 16; ++ks) {
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_k(buf, 0, u * 32, ks), kf[ks], s, 0, 0, 0);
+          dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_k(buf, TB, u * 32, ks), vf[ks], dp, 0, 0, 0);
         }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c, shut));
+          dp[r] *= s[r];                               // dS
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const bf16x8 pb = pack8(s, h), dsb = pack8(dp, h);
+#pragma unroll
+          for (int dt = 0; dt < D / 32; ++dt) {
+            dv[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_tr(buf, TB, dt, 32 * u + 16 * h), pb, dv[dt], 0, 0, 0);
+            dk[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr.frag_tr(buf, 0, dt, 32 * u + 16 * h), dsb, dk[dt], 0, 0, 0);
+          }
+        }
+        if (D == 128) __builtin_amdgcn_sched_barrier(0);
       }
     }
     if (t + 1 < nt) stash_stats(slot ^ 1);
     wait_tiles<0>();
     __syncthreads();
+  }
+  if (key >= len) {                               // a NaN in a row must not reach them either
+    clear(dk);
+    clear(dv);
   }
   if (a.splits > 1) {
     if (key < a.sk) {
