@@ -20,7 +20,8 @@ namespace bamboo {
 namespace {
 
 // exp(t) for t <= 0: the product with log2 e in two parts, whose rounding would otherwise shift every term the same way
-constexpr float kL2e = 1.4426950408889634f, kL2eRest = 1.9259629911266175e-8f;
+constexpr float kL2e = 1.4426950408889634f, kL2eRest = 1.9259629911266175e-8f, kLn2 = 0.6931471805599453f;
+constexpr float kFar = -300.f;      // an exponent of 2 whose power is 0
 __device__ __forceinline__ float exp_of(float t) { return __builtin_amdgcn_exp2f(fmaf(t, kL2eRest, t * kL2e)); }
 
 // 16 bytes of a row, at any alignment of an element (the rows of a vocabulary that divides by nothing start anywhere)
@@ -42,9 +43,15 @@ template <typename T> __device__ __forceinline__ typename Chunk<T>::type load_ch
   for (int j = 0; j < Chunk<T>::N; ++j) x[j] = v + j < V ? row[v + j] : (T)(-INFINITY);    // adds nothing
   return x;
 }
-template <typename T> __device__ __forceinline__ void store_chunk(T* row, int v, int V, typename Chunk<T>::type x) {
+// STREAM: not to be kept in the caches.  Gradients that do not fit there any more would only push out the logits that are still
+// to be read (4096 x 30528, of which half count: log-probabilities 40 us behind gradients that are kept, 23 behind streamed
+// ones; the gradients 53 and 51 us; policy loss of 4096 x 50304 144 and 138 us).
+template <typename T, bool STREAM>
+__device__ __forceinline__ void store_chunk(T* row, int v, int V, typename Chunk<T>::type x) {
   if (v + Chunk<T>::N <= V) {
-    *(typename Chunk<T>::loose*)(row + v) = x;
+    auto* p = (typename Chunk<T>::loose*)(row + v);
+    if (STREAM) __builtin_nontemporal_store((typename Chunk<T>::loose)x, p);
+    else *p = x;
     return;
   }
 #pragma unroll
@@ -79,38 +86,64 @@ template <int NT> __device__ __forceinline__ void block_sum2(float* a, float* b,
 }
 __device__ __forceinline__ int clamp_label(int id, int V) { return id < 0 ? 0 : (id >= V ? V - 1 : id); }
 
-// What a row's pass leaves: its maximum (0 in the place of -inf), the sum and its log, logp of the label, entropy.
-struct RowStats { float top, sum, log_s, at_label, logp, entropy; };
+// What a row's pass leaves.  e_v below is 2^(z_v log2 e - m2) with m2 = round(max log2 e), one multiply-add and the
+// exponential: what m2 is off by shifts all e_v and their sum alike, so that p_v = e_v / sum is free of it; from the sum's
+// logarithm it is taken back (`slip`).  (What log2 e is off by, 1e-8 of the distance to the maximum, stays.)
+struct RowStats {
+  float top, m2;           // maximum (0 in the place of -inf)
+  float sum, log_s, slip;  // of e_v; log of the sum of exp(z_v - top), = log(sum) - slip
+  float at_label, logp, entropy;
+  bool far;                // logits so far below the maximum that the distance is -inf
+};
 
-// NC > 0: the row lies in registers, NC chunks a thread.  NC = 0: it is read as often as it is needed.
-// A NaN or +inf in a row, or a row of -inf alone, makes its results NaN; other -inf add nothing.
+// NC > 0: the row lies in registers, NC chunks a thread; in fp32 the e_v take the logits' place.  NC = 0: it is read as
+// often as it is needed.  A NaN or +inf in a row, or a row of -inf alone, makes its results NaN; other -inf add nothing.
 template <typename T, int NT, int NC, bool ENT>
 struct RowPass {
   typedef typename Chunk<T>::type vec;
   static constexpr int E = Chunk<T>::N, HELD = NC > 0 ? NC : 1;
+  static constexpr bool KEEPS_EXP = NC > 0 && sizeof(T) == 4;
   vec x[HELD];
   __device__ __forceinline__ static int place(int c) { return (c * NT + (int)threadIdx.x) * E; }
   __device__ __forceinline__ RowStats run(const T* row, int V, int label, float* red) {
-    const float at_label = to_f32<T>(row[label]);
+    RowStats r;
+    r.at_label = to_f32<T>(row[label]);
     float m = -INFINITY, s = 0.f, w = 0.f;
-    bool bad = false;
     if constexpr (NC > 0) {
 #pragma unroll
       for (int c = 0; c < NC; ++c)
         if (place(c) < V) x[c] = load_chunk<T>(row, place(c), V);
+      centre(&r, block_max<NT>(own_max(V), red));
 #pragma unroll
       for (int c = 0; c < NC; ++c)
         if (place(c) < V)
 #pragma unroll
-          for (int j = 0; j < E; ++j) m = fmaxf(m, to_f32<T>(x[c][j]));
-      m = block_max<NT>(m, red);
-      const float from = m == -INFINITY ? 0.f : m;
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-        if (place(c) < V) add(x[c], from, &s, &w);
+          for (int j = 0; j < E; ++j) {
+            const float t = fmaf(to_f32<T>(x[c][j]), kL2e, -r.m2), e = __builtin_amdgcn_exp2f(t);
+            s += e;
+            if (ENT) w = fmaf(e, t, w);
+            if constexpr (KEEPS_EXP) x[c][j] = e;
+          }
       block_sum2<NT>(&s, &w, red + NT / 64);
-      m = from;
+      r.far = ENT && w != w && s == s;                            // 0 * -inf somewhere: the same for the whole workgroup
+      if (r.far) {
+        w = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+          if (place(c) < V)
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+              float t, e;
+              term(x[c], j, r, &t, &e);
+              w = fmaf(e, fmaxf(t, kFar), w);
+            }
+        float none = 0.f;
+        __syncthreads();
+        block_sum2<NT>(&w, &none, red + NT / 64);
+      }
     } else {
+      r.far = true;
+      // a thread's sums are of exp(z - m) and of that times (z - m), for its own running maximum m
       for (int c0 = 0; place(c0) < V; c0 += 4) {
         vec y[4];
 #pragma unroll
@@ -128,88 +161,135 @@ struct RowPass {
             s *= by;
             m = top;
           }
-          add(y[q], m == -INFINITY ? 0.f : m, &s, &w);
+          const float from = m == -INFINITY ? 0.f : m;
+#pragma unroll
+          for (int j = 0; j < E; ++j) {
+            const float t = to_f32<T>(y[q][j]) - from, e = exp_of(t);
+            s += e;
+            if (ENT) w = fmaf(e, fmaxf(t, kFar), w);
+          }
         }
       }
-      const float top = block_max<NT>(m, red);
-      const float from = top == -INFINITY ? 0.f : top;
-      const float away = m - from, by = exp_of(away);
-      if (m == -INFINITY) {
-        bad = s != 0.f;                                           // NaN among -inf
-        s = w = bad ? NAN : 0.f;
+      centre(&r, block_max<NT>(m, red));
+      if (m == -INFINITY) {                                       // nothing above -inf here: 0, or NaN
+        w = s;
       } else {
+        const float away = m - r.top, by = exp_of(away);
         if (ENT) w = by > 0.f ? by * (w + away * s) : 0.f;
         s *= by;
       }
       block_sum2<NT>(&s, &w, red + NT / 64);
-      m = from;
+      // in the units of the other form
+      const float shift = __builtin_amdgcn_exp2f(r.slip * kL2e);
+      if (ENT) w = (w * kL2e + r.slip * kL2e * s) * shift;
+      s *= shift;
     }
-    RowStats r;
-    r.top = m;
     r.sum = s;
-    r.at_label = at_label;
-    r.log_s = s > 0.f ? logf(s) : NAN;                            // a row of -inf alone, or a NaN in it
-    r.logp = (at_label - m) - r.log_s;
-    r.entropy = ENT ? r.log_s - w / s : 0.f;
+    const float l = s > 0.f ? logf(s) : NAN;                      // a row of -inf alone, or a NaN in it
+    r.log_s = l - r.slip;
+    r.logp = (r.at_label - r.top) - r.log_s;
+    r.entropy = ENT ? l - kLn2 * w / s : 0.f;
     return r;
   }
-  // sums of exp(z - from) and, for the entropy, of exp(z - from) (z - from)
-  __device__ __forceinline__ static void add(const vec& v, float from, float* s, float* w) {
-#pragma unroll
-    for (int j = 0; j < E; ++j) {
-      const float t = to_f32<T>(v[j]) - from, e = exp_of(t);
-      *s += e;
-      if (ENT) *w += e > 0.f ? e * t : 0.f;                       // 0 * -inf is 0 here
+  // of element j of a chunk: the exponent, and e_v
+  __device__ __forceinline__ static void term(const vec& v, int j, const RowStats& r, float* t, float* e) {
+    if constexpr (KEEPS_EXP) {
+      *e = v[j];
+      *t = __builtin_amdgcn_logf(*e);
+    } else {
+      *t = fmaf(to_f32<T>(v[j]), kL2e, -r.m2);
+      *e = __builtin_amdgcn_exp2f(*t);
     }
+  }
+  // Maximum of the thread's part of the row.  bf16: as integers of 16 bits, two at a time, numbers from 0 up are in order and
+  // above all negative ones, so the largest is found there unless there are none but negative ones.
+  __device__ __forceinline__ float own_max(int V) const {
+    if constexpr (sizeof(T) == 2) {
+      typedef short short2_t __attribute__((ext_vector_type(2)));
+      short2_t top = {(short)-32768, (short)-32768};
+#pragma unroll
+      for (int c = 0; c < HELD; ++c)
+        if (place(c) < V) {
+          union { vec v; short2_t p[4]; } u;
+          u.v = x[c];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, u.p[j]);
+        }
+      const short most = top[0] > top[1] ? top[0] : top[1];
+      if (most >= 0) return __builtin_bit_cast(float, (unsigned)(unsigned short)most << 16);
+    }
+    float m = -INFINITY;
+#pragma unroll
+    for (int c = 0; c < HELD; ++c)
+      if (place(c) < V)
+#pragma unroll
+        for (int j = 0; j < E; ++j) m = fmaxf(m, to_f32<T>(x[c][j]));
+    return m;
+  }
+  __device__ __forceinline__ static void centre(RowStats* r, float top) {
+    r->top = top == -INFINITY ? 0.f : top;
+    r->m2 = r->top * kL2e;
+    r->slip = (fmaf(r->top, kL2e, -r->m2) + r->top * kL2eRest) * kLn2;
   }
 };
 
 // d = scale * (coef * [v = label] + p_v * (ent * (log p_v + H) - coef))
-template <typename T, int NT, int NC, bool ENT>
-__device__ __forceinline__ void write_gradient(RowPass<T, NT, NC, ENT>& pass, const T* row, T* out, int V, int label,
+template <typename T, int NT, int NC, bool ENT, bool STREAM>
+__device__ __forceinline__ void write_gradient(const RowPass<T, NT, NC, ENT>& pass, const T* row, T* out, int V, int label,
                                                const RowStats& r, float coef, float ent, float scale) {
   typedef typename Chunk<T>::type vec;
   constexpr int E = Chunk<T>::N;
-  auto one = [&](int v, const vec& x) {
-    vec o;
+  const float per = scale / r.sum, hit = coef * scale;
+  const float k1 = ent * per * kLn2, k0 = (ent * (r.entropy - (r.log_s + r.slip)) - coef) * per;      // of t, and without it
+  auto write = [&](auto with_log, auto far) {
+    auto one = [&](int v, const vec& x) {
+      float d[E];
 #pragma unroll
-    for (int j = 0; j < E; ++j) {
-      const float lp = (to_f32<T>(x[j]) - r.top) - r.log_s;
-      const float p = exp_of(lp);
-      float k = -coef;
-      if (ENT) k = p > 0.f ? fmaf(ent, lp + r.entropy, -coef) : -coef;
-      const float hit = v + j == label ? coef : 0.f;
-      o[j] = from_f32<T>(fmaf(p, k, hit) * scale);
+      for (int j = 0; j < E; ++j) {
+        float t, e;
+        RowPass<T, NT, NC, ENT>::term(x, j, r, &t, &e);
+        d[j] = e * (with_log ? fmaf(k1, far ? fmaxf(t, kFar) : t, k0) : k0);
+      }
+      if ((unsigned)(label - v) < (unsigned)E) {                  // one chunk of the row
+#pragma unroll
+        for (int j = 0; j < E; ++j) d[j] += v + j == label ? hit : 0.f;
+      }
+      vec o;
+#pragma unroll
+      for (int j = 0; j < E; ++j) o[j] = from_f32<T>(d[j]);
+      store_chunk<T, STREAM>(out, v, V, o);
+    };
+    if constexpr (NC > 0) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int v = pass.place(c);
+        if (v < V) one(v, pass.x[c]);
+      }
+    } else {
+      for (int v = threadIdx.x * E; v < V; v += NT * E) one(v, load_chunk<T>(row, v, V));
     }
-    store_chunk<T>(out, v, V, o);
   };
-  if constexpr (NC > 0) {
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int v = pass.place(c);
-      if (v < V) one(v, pass.x[c]);
-    }
-  } else {
-    for (int v = threadIdx.x * E; v < V; v += NT * E) one(v, load_chunk<T>(row, v, V));
-  }
+  if (!ENT || ent == 0.f) write(std::false_type(), std::false_type());
+  else if (r.far) write(std::true_type(), std::true_type());
+  else write(std::true_type(), std::false_type());
 }
 
-template <typename T, int NT>
+template <typename T, int NT, bool STREAM>
 __device__ __forceinline__ void write_zeros(T* out, int V) {
   typename Chunk<T>::type o;
 #pragma unroll
   for (int j = 0; j < Chunk<T>::N; ++j) o[j] = (T)0.f;
-  for (int v = threadIdx.x * Chunk<T>::N; v < V; v += NT * Chunk<T>::N) store_chunk<T>(out, v, V, o);
+  for (int v = threadIdx.x * Chunk<T>::N; v < V; v += NT * Chunk<T>::N) store_chunk<T, STREAM>(out, v, V, o);
 }
 
 // One workgroup per token.
-template <typename T, int NT, int NC, bool ENT>
+template <typename T, int NT, int NC, bool ENT, bool STREAM>
 __global__ __launch_bounds__(NT) void policy_loss_kernel(PolicyDesc a) {
   __shared__ float red[3 * NT / 64];
   const long t = blockIdx.x;
   T* out = a.dlogits != nullptr ? (T*)a.dlogits + t * a.ldd : nullptr;
   if (a.mask != nullptr && a.mask[t] == 0) {          // uniform over the workgroup: nothing of the row is read
-    if (out != nullptr) write_zeros<T, NT>(out, a.V);
+    if (out != nullptr) write_zeros<T, NT, STREAM>(out, a.V);
     if (threadIdx.x == 0) {
       a.logp[t] = 0.f;
       a.loss_tok[t] = 0.f;
@@ -241,12 +321,12 @@ __global__ __launch_bounds__(NT) void policy_loss_kernel(PolicyDesc a) {
     if (a.kl_tok != nullptr) a.kl_tok[t] = kl;
     if (ENT && a.entropy != nullptr) a.entropy[t] = r.entropy;
   }
-  if (out != nullptr) write_gradient<T, NT, NC, ENT>(pass, row, out, a.V, label, r, coef, a.ent_coef, a.scale);
+  if (out != nullptr) write_gradient<T, NT, NC, ENT, STREAM>(pass, row, out, a.V, label, r, coef, a.ent_coef, a.scale);
 }
 
 // lse and the label's log-probability of every token that counts (0 for the others).  The latter in 64 bits too: the margin
 // is a small difference of two sums over sequences, and roundings of each term, a few 10^-7, would be most of its error.
-template <typename T, int NT, int NC>
+template <typename T, int NT>
 __global__ __launch_bounds__(NT) void token_logp_kernel(PreferenceDesc a) {
   __shared__ float red[3 * NT / 64];
   const long t = blockIdx.x;
@@ -257,12 +337,12 @@ __global__ __launch_bounds__(NT) void token_logp_kernel(PreferenceDesc a) {
     }
     return;
   }
-  RowPass<T, NT, NC, false> pass;
+  RowPass<T, NT, 0, false> pass;
   const RowStats r = pass.run((const T*)a.logits + t * a.ldl, a.V, clamp_label(a.labels[t], a.V), red);
   if (threadIdx.x == 0) {
     a.lse[t] = r.top + r.log_s;
     a.logp[t] = r.logp;
-    a.scratch[t] = ((double)r.at_label - r.top) - (r.sum > 0.f ? log((double)r.sum) : NAN);
+    a.scratch[t] = ((double)r.at_label - r.top) - (r.sum > 0.f ? log((double)r.sum) - r.slip : NAN);
   }
 }
 
@@ -271,24 +351,34 @@ __device__ __forceinline__ double softplus(double x) { return x > 0 ? x + log1p(
 
 // Per pair: sums of both sequences' log-probabilities (64 bits, fixed order), margin and loss.
 __global__ __launch_bounds__(256) void pair_loss_kernel(PreferenceDesc a) {
-  __shared__ double red[2][256];
+  __shared__ double red[2][4];
   const int i = blockIdx.x;
+  const double *lc = a.scratch + (long)i * a.seq, *lr = lc + (long)a.pairs * a.seq;
+  double sc = 0., sr = 0.;
+  for (int t = threadIdx.x; t < a.seq; t += 1024) {
+    double x[4], y[4];
 #pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    const double* lp = a.scratch + ((long)side * a.pairs + i) * a.seq;
-    double s = 0.;
-    for (int t = threadIdx.x; t < a.seq; t += 256) s += lp[t];
-    red[side][threadIdx.x] = s;
+    for (int q = 0; q < 4; ++q) {
+      x[q] = t + 256 * q < a.seq ? lc[t + 256 * q] : 0.;
+      y[q] = t + 256 * q < a.seq ? lr[t + 256 * q] : 0.;
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      sc += x[q];
+      sr += y[q];
+    }
+  }
+  for (int o = 32; o > 0; o >>= 1) {
+    sc += __shfl_xor(sc, o, 64);
+    sr += __shfl_xor(sr, o, 64);
+  }
+  if ((threadIdx.x & 63) == 0) {
+    red[0][threadIdx.x >> 6] = sc;
+    red[1][threadIdx.x >> 6] = sr;
   }
   __syncthreads();
-  for (int o = 128; o > 0; o >>= 1) {
-    if ((int)threadIdx.x < o)
-#pragma unroll
-      for (int side = 0; side < 2; ++side) red[side][threadIdx.x] += red[side][threadIdx.x + o];
-    __syncthreads();
-  }
   if (threadIdx.x == 0) {
-    const double c = red[0][0], r = red[1][0];
+    const double c = (red[0][0] + red[0][1]) + (red[0][2] + red[0][3]), r = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
     const double margin = (double)a.beta * ((c - a.ref_logp[i]) - (r - a.ref_logp[a.pairs + i]));
     a.logp_seq[i] = (float)c;
     a.logp_seq[a.pairs + i] = (float)r;
@@ -297,40 +387,50 @@ __global__ __launch_bounds__(256) void pair_loss_kernel(PreferenceDesc a) {
   }
 }
 
-// dlogits = scale * dL/dlogp_seq * ([v = label] - p), dL/dlogp_seq = +-beta (sigmoid(margin) - (1 - smoothing))
-template <typename T>
+// dlogits = scale * dL/dlogp_seq * ([v = label] - p), dL/dlogp_seq = +-beta (sigmoid(margin) - (1 - smoothing)).
+// A workgroup takes four chunks a thread of a row: no thread needs another's, and the rows of a short batch fill the chip.
+constexpr int kAhead = 4;
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void preference_bwd_kernel(PreferenceDesc a) {
   typedef typename Chunk<T>::type vec;
-  constexpr int E = Chunk<T>::N, AHEAD = 4;
+  constexpr int E = Chunk<T>::N;
   const long t = blockIdx.x;
+  const int v0 = (int)(blockIdx.y * kAhead * 256 + threadIdx.x) * E;
   T* out = (T*)a.dlogits + t * a.ldd;
   if (a.mask != nullptr && a.mask[t] == 0) {
-    write_zeros<T, 256>(out, a.V);
+    vec o;
+#pragma unroll
+    for (int j = 0; j < E; ++j) o[j] = (T)0.f;
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q)
+      if (v0 + q * 256 * E < a.V) store_chunk<T, STREAM>(out, v0 + q * 256 * E, a.V, o);
     return;
   }
   const T* row = (const T*)a.logits + t * a.ldl;
+  vec x[kAhead];
+#pragma unroll
+  for (int q = 0; q < kAhead; ++q)
+    if (v0 + q * 256 * E < a.V) x[q] = load_chunk<T>(row, v0 + q * 256 * E, a.V);
   const int label = clamp_label(a.labels[t], a.V);
   const int seq = (int)(t / a.seq), pair = seq < a.pairs ? seq : seq - a.pairs;
+  const float lse = a.lse[t];
   const double g = 1. / (1. + exp(-(double)a.margin[pair])) - (1. - (double)a.smoothing);
   const float coef = (float)((seq < a.pairs ? g : -g) * (double)a.beta * (double)a.scale);
-  const float lse = a.lse[t];
-  for (int v0 = threadIdx.x * E; v0 < a.V; v0 += AHEAD * 256 * E) {
-    vec x[AHEAD];
 #pragma unroll
-    for (int q = 0; q < AHEAD; ++q)
-      if (v0 + q * 256 * E < a.V) x[q] = load_chunk<T>(row, v0 + q * 256 * E, a.V);
+  for (int q = 0; q < kAhead; ++q) {
+    const int v = v0 + q * 256 * E;
+    if (v >= a.V) break;
+    float d[E];
 #pragma unroll
-    for (int q = 0; q < AHEAD; ++q) {
-      const int v = v0 + q * 256 * E;
-      if (v >= a.V) break;
-      vec o;
+    for (int j = 0; j < E; ++j) d[j] = -coef * exp_of(to_f32<T>(x[q][j]) - lse);
+    if ((unsigned)(label - v) < (unsigned)E) {
 #pragma unroll
-      for (int j = 0; j < E; ++j) {
-        const float p = exp_of(to_f32<T>(x[q][j]) - lse);
-        o[j] = from_f32<T>(coef * ((v + j == label ? 1.f : 0.f) - p));
-      }
-      store_chunk<T>(out, v, a.V, o);
+      for (int j = 0; j < E; ++j) d[j] += v + j == label ? coef : 0.f;
     }
+    vec o;
+#pragma unroll
+    for (int j = 0; j < E; ++j) o[j] = from_f32<T>(d[j]);
+    store_chunk<T, STREAM>(out, v, a.V, o);
   }
 }
 
@@ -338,33 +438,42 @@ __global__ __launch_bounds__(256) void preference_bwd_kernel(PreferenceDesc a) {
 template <typename T, typename GO>
 hipError_t by_row_length(int V, GO go) {
   const int chunks = (V + Chunk<T>::N - 1) / Chunk<T>::N;
-  if (chunks <= 256) return go(std::integral_constant<int, 256>(), std::integral_constant<int, 1>());
-  if (chunks <= 512) return go(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
-  if (chunks <= 1024) return go(std::integral_constant<int, 256>(), std::integral_constant<int, 4>());
-  if (chunks <= 2048) return go(std::integral_constant<int, 256>(), std::integral_constant<int, 8>());
-  if (chunks <= 4096) return go(std::integral_constant<int, 512>(), std::integral_constant<int, 8>());
-  if (chunks <= 8192) return go(std::integral_constant<int, 1024>(), std::integral_constant<int, 8>());
-  if (chunks <= 16384) return go(std::integral_constant<int, 1024>(), std::integral_constant<int, 16>());
+#define BAMBOO_ROW(NT, NC) \
+  if (chunks <= NT * NC) return go(std::integral_constant<int, NT>(), std::integral_constant<int, NC>())
+  BAMBOO_ROW(256, 1);
+  BAMBOO_ROW(256, 2);
+  BAMBOO_ROW(256, 4);
+  BAMBOO_ROW(256, 6);
+  BAMBOO_ROW(256, 8);
+  BAMBOO_ROW(256, 12);
+  BAMBOO_ROW(256, 16);
+  BAMBOO_ROW(512, 10);
+  BAMBOO_ROW(512, 13);
+  BAMBOO_ROW(512, 16);
+  BAMBOO_ROW(1024, 12);
+  BAMBOO_ROW(1024, 16);
+#undef BAMBOO_ROW
   return go(std::integral_constant<int, 1024>(), std::integral_constant<int, 0>());
 }
 
 template <typename T>
 hipError_t policy_launch(hipStream_t s, const PolicyDesc& a) {
+  const bool stream = streams_past_cache(2L * a.T * a.V * (long)sizeof(T));
   return by_row_length<T>(a.V, [&](auto nt, auto nc) {
     constexpr int NT = decltype(nt)::value, NC = decltype(nc)::value;
-    const auto kern = a.entropy != nullptr || a.ent_coef != 0.f ? policy_loss_kernel<T, NT, NC, true>
-                                                                : policy_loss_kernel<T, NT, NC, false>;
+    const bool ent = a.entropy != nullptr || a.ent_coef != 0.f;
+    const auto kern = ent ? (stream ? policy_loss_kernel<T, NT, NC, true, true> : policy_loss_kernel<T, NT, NC, true, false>)
+                          : (stream ? policy_loss_kernel<T, NT, NC, false, true> : policy_loss_kernel<T, NT, NC, false, false>);
     hipLaunchKernelGGL(kern, dim3((unsigned)a.T), dim3(NT), 0, s, a);
     return hipGetLastError();
   });
 }
+// Read once, so nothing is held.  Few rows: their time is a chain of trips to memory, fewer with more threads.
 template <typename T>
 hipError_t token_logp_launch(hipStream_t s, const PreferenceDesc& a, unsigned rows) {
-  return by_row_length<T>(a.V, [&](auto nt, auto nc) {
-    constexpr int NT = decltype(nt)::value, NC = decltype(nc)::value;
-    hipLaunchKernelGGL((token_logp_kernel<T, NT, NC>), dim3(rows), dim3(NT), 0, s, a);
-    return hipGetLastError();
-  });
+  if (rows >= 512) hipLaunchKernelGGL((token_logp_kernel<T, 256>), dim3(rows), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((token_logp_kernel<T, 1024>), dim3(rows), dim3(1024), 0, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -383,8 +492,12 @@ hipError_t launch_preference_fwd(hipStream_t s, int dtype, const PreferenceDesc&
 
 hipError_t launch_preference_bwd(hipStream_t s, int dtype, const PreferenceDesc& a) {
   const unsigned rows = 2u * (unsigned)a.pairs * (unsigned)a.seq;
-  if (dtype == 1) hipLaunchKernelGGL(preference_bwd_kernel<bf16_t>, dim3(rows), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(preference_bwd_kernel<float>, dim3(rows), dim3(256), 0, s, a);
+  const bool stream = streams_past_cache(2L * rows * a.V * (dtype == 1 ? 2 : 4));
+  const int per = kAhead * 256 * (dtype == 1 ? Chunk<bf16_t>::N : Chunk<float>::N);
+  const dim3 grid(rows, (unsigned)((a.V + (long)per - 1) / per));
+  const auto kern = dtype == 1 ? (stream ? preference_bwd_kernel<bf16_t, true> : preference_bwd_kernel<bf16_t, false>)
+                               : (stream ? preference_bwd_kernel<float, true> : preference_bwd_kernel<float, false>);
+  hipLaunchKernelGGL(kern, grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
