@@ -152,8 +152,8 @@ int bk_rotary_frequencies(int rot, double base, int scaling, double factor, int 
  * and values behind them are never read.  ctx[batch*sq, heads*d] (row stride ldc), lse[batch,heads,sq] fp32.  A sample
  * without keys has ctx = 0 and lse = -inf.
  * scratch: fp32, bk_cross_attention_scratch_floats(..) floats, 16-byte aligned, used by this call alone.
- * impl: 0 automatic, 1 fp32 arithmetic on the matrix cores (any d and alignment), 2 bf16 (BAMBOO_E_STATE if it does not
- * cover the shape: bf16, d 64 or 128, strides multiples of 8, pointers 16-byte aligned). */
+ * impl: 0 automatic, 1 fp32 arithmetic on the matrix cores, 2 bf16 on them (BAMBOO_E_STATE for fp32 tensors).  bf16 is fastest
+ * with d 64 or 128, strides multiples of 8 and pointers aligned to 16 bytes. */
 int bk_cross_attention_fwd(int dtype, int impl, int batch, int sq, int sk, int heads, int kv_heads, int d, const void* q,
                            int64_t ldq, const void* k, const void* v, int64_t ldkv, const int32_t* kv_len, void* ctx,
                            int64_t ldc, float* lse, float* scratch, void* stream);

@@ -356,13 +356,12 @@ struct CrossDesc {
   int rows, group, splits;
   unsigned group_inv;
   float *part, *part_stats, *delta;
+  long part_stride;        // floats between the parts of a gradient, a multiple of 4
 };
 uint64_t cross_attention_scratch_floats(int B, int sq, int sk, int heads, int kv_heads, int d);
 hipError_t launch_cross_attention_fwd(hipStream_t s, int dtype, int impl, const CrossDesc& d);
 hipError_t launch_cross_attention_bwd(hipStream_t s, int dtype, int impl, const CrossDesc& d);
-// the passes, with everything set: bf16 on the matrix cores (head size 64 or 128), and any head size up to 128 in fp32
-// arithmetic on them
-bool cross_mfma_covers(const CrossDesc& d);
+// the passes, with everything set: bf16 on the matrix cores, and both types in fp32 arithmetic on them
 hipError_t launch_cross_fwd_mfma(hipStream_t s, const CrossDesc& d);
 hipError_t launch_cross_dq_mfma(hipStream_t s, const CrossDesc& d);
 hipError_t launch_cross_dkv_mfma(hipStream_t s, const CrossDesc& d);

@@ -61,61 +61,94 @@ __global__ __launch_bounds__(256) void cross_join_fwd_kernel(CrossDesc a) {
   if (lane == 0) a.lse[cross_stat(a, b, at)] = cross_len(a, b) > 0 ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
 }
 
-// Gradients: sums of the parts in order.  One thread an element; KEYS: dk and dv, otherwise dq.
+// Gradients: sums of the parts in order.  A thread takes four elements and has eight parts in flight (one element and part at a
+// time: 32 parts of 256 keys x 128 took 61 us); the parts are `stride` floats apart, a multiple of 4.  KEYS: dk and dv,
+// otherwise dq.
 template <typename T, bool KEYS>
-__global__ __launch_bounds__(256) void cross_join_bwd_kernel(CrossDesc a) {
+__global__ __launch_bounds__(256) void cross_join_bwd_kernel(CrossDesc a, long n, long stride) {
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
   const int per = KEYS ? a.sk : a.rows, cols = KEYS ? 2 * a.d : a.d;
-  const long n = (long)a.B * a.kv_heads * per * cols, i = (long)blockIdx.x * 256 + threadIdx.x;
+  const long i = ((long)blockIdx.x * 256 + threadIdx.x) * 4;
   if (i >= n) return;
-  float x = 0.f;
-  for (int s = 0; s < a.splits; ++s) x += a.part[s * n + i];
-  const int c = (int)(i % cols);
-  const long row = i / cols;
-  const int pair = (int)(row / per), r = (int)(row % per), b = pair / a.kv_heads, kvh = pair % a.kv_heads;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < a.splits; s += 8) {
+    f32x4 p[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) p[q] = *(const f32x4*)(a.part + min(s + q, a.splits - 1) * stride + i);
+#pragma unroll
+    for (int q = 0; q < 8; ++q)
+      if (s + q < a.splits) x += p[q];
+  }
   const float scale = rsqrtf((float)a.d);
-  if (KEYS) {
-    const long out = ((long)b * a.sk + r) * a.lddkv + (long)kvh * a.d;
-    if (c < a.d) ((T*)a.dk)[out + c] = from_f32<T>(x * scale);
-    else ((T*)a.dv)[out + c - a.d] = from_f32<T>(x);
-  } else {
-    const CrossRow at = cross_row(a, kvh, r);
-    ((T*)a.dq)[((long)b * a.sq + at.query) * a.lddq + (long)at.head * a.d + c] = from_f32<T>(x * scale);
+  long row = i / cols;
+  int c = (int)(i % cols);
+#pragma unroll
+  for (int j = 0; j < 4; ++j, ++c) {
+    if (i + j >= n) break;
+    if (c == cols) {
+      c = 0;
+      ++row;
+    }
+    const int pair = (int)(row / per), r = (int)(row % per), b = pair / a.kv_heads, kvh = pair % a.kv_heads;
+    if (KEYS) {
+      const long out = ((long)b * a.sk + r) * a.lddkv + (long)kvh * a.d;
+      if (c < a.d) ((T*)a.dk)[out + c] = from_f32<T>(x[j] * scale);
+      else ((T*)a.dv)[out + c - a.d] = from_f32<T>(x[j]);
+    } else {
+      const CrossRow at = cross_row(a, kvh, r);
+      ((T*)a.dq)[((long)b * a.sq + at.query) * a.lddq + (long)at.head * a.d + c] = from_f32<T>(x[j] * scale);
+    }
   }
 }
 template <bool KEYS>
 hipError_t join_bwd(hipStream_t s, int dtype, const CrossDesc& a) {
   const long n = (long)a.B * a.kv_heads * (KEYS ? 2L * a.sk : (long)a.rows) * a.d;
-  const dim3 grid((unsigned)((n + 255) / 256));
-  if (dtype == 1) hipLaunchKernelGGL((cross_join_bwd_kernel<bf16_t, KEYS>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((cross_join_bwd_kernel<float, KEYS>), grid, dim3(256), 0, s, a);
+  const dim3 grid((unsigned)((n + 1023) / 1024));
+  if (dtype == 1) hipLaunchKernelGGL((cross_join_bwd_kernel<bf16_t, KEYS>), grid, dim3(256), 0, s, a, n, a.part_stride);
+  else hipLaunchKernelGGL((cross_join_bwd_kernel<float, KEYS>), grid, dim3(256), 0, s, a, n, a.part_stride);
   return hipGetLastError();
 }
 
+long up4(long n) { return (n + 3) / 4 * 4; }
+
 // Parts of the streamed side (`streamed` rows) for `owned` rows of each of `pairs` problems: one where the owned rows give
-// every CU a workgroup, otherwise as many as make two workgroups a CU, of four tiles at least.
-int parts(long owned, long streamed, long pairs) {
+// every CU a workgroup, otherwise as many as make two a CU, of `least` tiles at least.  A part's results (`floats`) are
+// written and read again, 8 bytes each at 5 TB/s, so that more than sqrt(time of all tiles / that) parts cost more than they
+// save.  `tile_us`: a tile of 64 rows.  dK and dV of 1 x 2048 x 4096, 96 heads over 8 of 128 (256 workgroups): 1018 us as one
+// part, 830 + 28 as two; of 8 x 512 x 333, 16 heads of 64 (384): 26 us as one, 35 + 20 as two.
+int parts(long owned, long streamed, long pairs, long floats, float tile_us, int least) {
   const long wgs = (owned + 127) / 128 * pairs, tiles = (streamed + 63) / 64;
-  if (wgs >= 512 || tiles < 8 || (wgs >= 256 && tiles < 64)) return 1;
+  if (wgs > 256) return 1;
   long n = (512 + wgs - 1) / wgs;
-  if (n > tiles / 4) n = tiles / 4;
+  if (n > tiles / least) n = tiles / least;
+  const float most = sqrtf(tiles * tile_us / (floats * 1.6e-6f));
+  if (n > most) n = (long)most;
   return (int)(n < 1 ? 1 : n);
 }
-long up4(long n) { return (n + 3) / 4 * 4; }
 
 struct Plan {
   int fwd, dq, dkv;                       // parts
   long fwd_floats, delta, dq_floats, dkv_floats;
 };
-Plan plan(int B, int sq, int sk, int heads, int kv_heads, int d) {
+Plan plan(bool mfma, int B, int sq, int sk, int heads, int kv_heads, int d) {
   const long pairs = (long)B * kv_heads, rows = (long)sq * (heads / kv_heads);
+  const long row_floats = pairs * rows * d, key_floats = 2 * pairs * (long)sk * d;
+  const float tile_us = mfma ? 0.4f + 0.008f * d : 0.5f + 0.05f * d;
+  const int least = mfma ? 4 : 1;
   Plan p;
-  p.fwd = p.dq = parts(rows, sk, pairs);
-  p.dkv = parts(sk, rows, pairs);
-  p.fwd_floats = p.fwd > 1 ? up4(p.fwd * pairs * rows * d) + up4(p.fwd * pairs * rows * 2) : 0;
+  p.fwd = parts(rows, sk, pairs, row_floats, tile_us, least);
+  p.dq = parts(rows, sk, pairs, row_floats, 1.5f * tile_us, least);
+  p.dkv = parts(sk, rows, pairs, key_floats, 2.f * tile_us, least);
+  p.fwd_floats = p.fwd > 1 ? up4(p.fwd * row_floats) + up4(p.fwd * pairs * rows * 2) : 0;
   p.delta = up4(pairs * rows);
-  p.dq_floats = p.dq > 1 ? up4(p.dq * pairs * rows * d) : 0;
-  p.dkv_floats = p.dkv > 1 ? up4(p.dkv * pairs * (long)sk * 2 * d) : 0;
+  p.dq_floats = p.dq > 1 ? p.dq * up4(row_floats) : 0;
+  p.dkv_floats = p.dkv > 1 ? p.dkv * up4(key_floats) : 0;
   return p;
+}
+long floats_of(const Plan& p) {
+  // the parts of one pass after the other in the same place, behind delta
+  const long bwd = p.delta + (p.dq_floats > p.dkv_floats ? p.dq_floats : p.dkv_floats);
+  return p.fwd_floats > bwd ? p.fwd_floats : bwd;
 }
 void shared_fields(CrossDesc& a) {
   a.group = a.heads / a.kv_heads;
@@ -126,21 +159,19 @@ void shared_fields(CrossDesc& a) {
 }  // namespace
 
 uint64_t cross_attention_scratch_floats(int B, int sq, int sk, int heads, int kv_heads, int d) {
-  const Plan p = plan(B, sq, sk, heads, kv_heads, d);
-  // the parts of one pass after the other in the same place, behind delta
-  const long parts_bwd = p.dq_floats > p.dkv_floats ? p.dq_floats : p.dkv_floats, bwd = p.delta + parts_bwd;
-  return (uint64_t)(p.fwd_floats > bwd ? p.fwd_floats : bwd);
+  const long x = floats_of(plan(true, B, sq, sk, heads, kv_heads, d)), y = floats_of(plan(false, B, sq, sk, heads, kv_heads, d));
+  return (uint64_t)(x > y ? x : y);
 }
 
 hipError_t launch_cross_attention_fwd(hipStream_t s, int dtype, int impl, const CrossDesc& d) {
   CrossDesc a = d;
   shared_fields(a);
-  const Plan p = plan(a.B, a.sq, a.sk, a.heads, a.kv_heads, a.d);
+  const bool mfma = impl != 1 && dtype == 1;
+  if (impl == 2 && !mfma) return hipErrorNotSupported;
+  const Plan p = plan(mfma, a.B, a.sq, a.sk, a.heads, a.kv_heads, a.d);
   a.splits = p.fwd;
   a.part = a.scratch;
   a.part_stats = a.scratch + up4(p.fwd * (long)a.B * a.kv_heads * a.rows * a.d);
-  const bool mfma = impl != 1 && dtype == 1 && cross_mfma_covers(a);
-  if (impl == 2 && !mfma) return hipErrorNotSupported;
   hipError_t e = mfma ? launch_cross_fwd_mfma(s, a) : launch_cross_fwd_f32(s, dtype, a);
   if (e != hipSuccess || a.splits == 1) return e;
   const dim3 grid((unsigned)(((long)a.B * a.kv_heads * a.rows + 3) / 4));
@@ -152,16 +183,18 @@ hipError_t launch_cross_attention_fwd(hipStream_t s, int dtype, int impl, const 
 hipError_t launch_cross_attention_bwd(hipStream_t s, int dtype, int impl, const CrossDesc& d) {
   CrossDesc a = d;
   shared_fields(a);
-  const Plan p = plan(a.B, a.sq, a.sk, a.heads, a.kv_heads, a.d);
+  const bool mfma = impl != 1 && dtype == 1;
+  if (impl == 2 && !mfma) return hipErrorNotSupported;
+  const Plan p = plan(mfma, a.B, a.sq, a.sk, a.heads, a.kv_heads, a.d);
   a.delta = a.scratch;
   a.part = a.scratch + p.delta;
-  const bool mfma = impl != 1 && dtype == 1 && cross_mfma_covers(a);
-  if (impl == 2 && !mfma) return hipErrorNotSupported;
   a.splits = p.dq;
+  a.part_stride = p.dq_floats / p.dq;
   hipError_t e = mfma ? launch_cross_dq_mfma(s, a) : launch_cross_dq_f32(s, dtype, a);
   if (e == hipSuccess && a.splits > 1) e = join_bwd<false>(s, dtype, a);
   if (e != hipSuccess) return e;
   a.splits = p.dkv;
+  a.part_stride = p.dkv_floats / p.dkv;
   e = mfma ? launch_cross_dkv_mfma(s, a) : launch_cross_dkv_f32(s, dtype, a);
   if (e == hipSuccess && a.splits > 1) e = join_bwd<true>(s, dtype, a);
   return e;

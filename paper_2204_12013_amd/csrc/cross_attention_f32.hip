@@ -266,8 +266,7 @@ __global__ __launch_bounds__(256, 1) void cross_dq_f32_kernel(CrossDesc a) {
   }
   if (!live) return;
   if (a.splits > 1) {
-    const long i = ((long)w.split * a.B * a.kv_heads + w.pair) * a.rows + row;
-    store_row<float, DP, VEC>(a.part + i * d, dq, 1.f, d);
+    store_row<float, DP, VEC>(a.part + w.split * a.part_stride + ((long)w.pair * a.rows + row) * d, dq, 1.f, d);
     return;
   }
   store_row<T, DP, VEC>((T*)a.dq + tok * a.lddq + (long)at.head * d, dq, scale, d);
@@ -335,9 +334,9 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_f32_kernel(CrossDesc a) {
   }
   if (key >= a.sk) return;
   if (a.splits > 1) {
-    const long i = (((long)w.split * a.B * a.kv_heads + w.pair) * a.sk + key) * 2;
-    store_row<float, DP, VEC>(a.part + i * d, dk, 1.f, d);
-    store_row<float, DP, VEC>(a.part + (i + 1) * d, dv, 1.f, d);
+    float* out = a.part + w.split * a.part_stride + ((long)w.pair * a.sk + key) * (2 * d);
+    store_row<float, DP, VEC>(out, dk, 1.f, d);
+    store_row<float, DP, VEC>(out + d, dv, 1.f, d);
     return;
   }
   const long out = ((long)w.b * a.sk + key) * a.lddkv + (long)w.kvh * d;
