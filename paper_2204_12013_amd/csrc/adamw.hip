@@ -26,7 +26,7 @@ namespace {
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 
-constexpr int kGroups = 2;                        // groups of 256 elements a wavefront takes
+constexpr int kGroups = 1;                        // groups of 256 elements a wavefront takes
 constexpr int kPerWg = 4 * kGroups * 256;
 
 template <bool STREAM> __device__ __forceinline__ f32x4 load4(const float* p) {
@@ -52,15 +52,16 @@ template <bool STREAM> __device__ __forceinline__ void put4(float* p, const f32x
   for (int j = 0; j < 4; ++j)
     if (64 * j + lane < left) p[64 * j + lane] = v[j];
 }
-__device__ __forceinline__ void put_storage(float* p, const f32x4& v, bool vec, int lane, int left) {
-  put4<false>(p, v, vec, lane, left);
+template <bool STREAM> __device__ __forceinline__ void put_storage(float* p, const f32x4& v, bool vec, int lane, int left) {
+  put4<STREAM>(p, v, vec, lane, left);
 }
-__device__ __forceinline__ void put_storage(bf16_t* p, const f32x4& v, bool vec, int lane, int left) {
+template <bool STREAM> __device__ __forceinline__ void put_storage(bf16_t* p, const f32x4& v, bool vec, int lane, int left) {
   if (vec) {
     bf16x4 t;
 #pragma unroll
     for (int j = 0; j < 4; ++j) t[j] = (bf16_t)v[j];
-    *(bf16x4*)(p + 4 * lane) = t;
+    if (STREAM) __builtin_nontemporal_store(t, (bf16x4*)(p + 4 * lane));
+    else *(bf16x4*)(p + 4 * lane) = t;
     return;
   }
 #pragma unroll
@@ -116,10 +117,10 @@ template <typename T, int BITS, bool STREAM>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamwBatch a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // this workgroup's tensor: the last whose first workgroup is not behind it
-  const bool here = lane < a.n && a.t[min(lane, kAdamwTensors - 1)].first_wg <= (int)blockIdx.x;
+  const bool here = lane < a.n && a.first_wg[min(lane, kAdamwTensors - 1)] <= (int)blockIdx.x;
   const int k = __popcll(__ballot(here)) - 1;
   const AdamwTensor& p = a.t[k];
-  const long start = (long)((int)blockIdx.x - p.first_wg) * kPerWg + wave * (kGroups * 256);
+  const long start = (long)((int)blockIdx.x - a.first_wg[k]) * kPerWg + wave * (kGroups * 256);
   const long n = p.numel;
   f32x4 g[kGroups], w[kGroups], m[kGroups], v[kGroups];
   bool vec[kGroups];
@@ -154,7 +155,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwBatch a) {
       w[u][j] = w[u][j] * p.keep - a.lr_c1 * m[u][j] / fmaf(root[j], a.root_c2, a.eps);
     }
     put4<STREAM>(p.master + at, w[u], vec[u], lane, left[u]);
-    put_storage((T*)p.w + at, w[u], vec[u], lane, left[u]);            // read by the next iteration
+    put_storage<STREAM>((T*)p.w + at, w[u], vec[u], lane, left[u]);
     if (BITS == 32) {
       put4<STREAM>((float*)p.m + at, m[u], vec[u], lane, left[u]);
       put4<STREAM>((float*)p.v + at, v[u], vec[u], lane, left[u]);
@@ -228,7 +229,7 @@ hipError_t launch_adamw(hipStream_t s, int dtype, int bits, const AdamwHyper& h,
       if (b.n > 0 && wgs + need > 0x7fffffffL) break;
       AdamwTensor& p = b.t[b.n++];
       p = t[i];
-      p.first_wg = (int)wgs;
+      b.first_wg[b.n - 1] = (int)wgs;
       p.keep = (float)(1. - h.lr * decay[i]);
       p.key = mix(run + (unsigned)i * 0x85ebca6bu);
       uintptr_t at = (uintptr_t)p.g | (uintptr_t)p.master;

@@ -380,9 +380,10 @@ struct AdamwTensor {
   long numel;
   float keep;              // 1 - lr decay
   unsigned key;            // of the tensor's rounding
-  int first_wg, aligned;
+  int aligned;
 };
 struct AdamwBatch {
+  int first_wg[kAdamwTensors];   // of each tensor: side by side, found with one load of a wavefront
   AdamwTensor t[kAdamwTensors];
   int n;
   float beta1, beta2, not_beta1, not_beta2, eps, lr_c1, root_c2;   // lr / (1 - beta1^step), 1 / sqrt(1 - beta2^step)
