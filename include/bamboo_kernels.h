@@ -125,7 +125,8 @@ int bk_ordered_sum(int64_t n, const float* in, float scale, float* out, void* st
 
 /* ---- operators of a training step around the stage: what a model that reads an encoder, or is trained further from
  * preferences or rewards, puts between the calls above.  Here a row of a matrix may be followed by other columns: ld* is
- * the distance between rows in elements.  Outputs must not overlap inputs except where it says so.  Calls work on the
+ * the distance between rows in elements.  Outputs must not overlap inputs or each other except where it says so
+ * (columns of one matrix beside each other do not).  Calls work on the
  * current device, which the stream and all pointers belong to; nothing is kept from one call for the next.
  *
  * Rotary positions, between the QKV product and the attention: in each of `heads` heads of row t (columns h*d .. h*d+d-1),
@@ -172,7 +173,7 @@ uint64_t bk_cross_attention_scratch_floats(int batch, int sq, int sk, int heads,
  * H: entropy of the token's distribution.  mask: device bytes [T], 0 = the token does not count (its logits are not read;
  * all it gets is zeros), or NULL.  ref_logp NULL: no KL term.  Any V, strides ldl, ldd in elements; labels outside [0, V) are
  * clamped.  Outputs [T] fp32: logp, loss_tok, and, unless NULL, kl_tok (the term without its coefficient) and entropy;
- * dlogits NULL: no gradient; dlogits may be logits (with ldd = ldl).  logits of -inf take no part; a NaN, +inf or a row
+ * dlogits NULL: no gradient; dlogits may be logits (with ldd = ldl).  V <= 2^27.  Logits of -inf take no part; a NaN, +inf or a row
  * of -inf alone makes the row NaN.  The mean over the tokens: bk_ordered_sum. */
 int bk_policy_loss(int dtype, int T, int V, const void* logits, int64_t ldl, const int32_t* labels, const uint8_t* mask,
                    const float* old_logp, const float* ref_logp, const float* adv, float clip_low, float clip_high,

@@ -233,16 +233,25 @@ int bk_ordered_sum(int64_t n, const float* in, float scale, float* out, void* st
 
 // ---- operators around the stage ----------------------------------------------
 
-// rows of `cols` elements of `es` bytes, ld elements apart
-struct Span { uintptr_t first, last; };
-static Span span_of(const void* p, int64_t rows, int64_t ld, int64_t cols, int es) {
-  return {(uintptr_t)p, (uintptr_t)p + (uintptr_t)(((rows - 1) * ld + cols) * es)};
+// A matrix in memory: rows of `cols` elements of `es` bytes, ld elements apart.
+struct Matrix {
+  const void* p;
+  int64_t rows, ld, cols;
+  int es;
+  uintptr_t first() const { return (uintptr_t)p; }
+  uintptr_t last() const { return (uintptr_t)p + (uintptr_t)(((rows - 1) * ld + cols) * es); }
+};
+// Whether two matrices share an element; columns of one matrix beside each other do not, nor does a matrix with itself, row
+// on row, where `itself` says that it may be there.
+static bool overlap(const Matrix& a, const Matrix& b, bool itself = false) {
+  if (a.first() >= b.last() || b.first() >= a.last()) return false;
+  const int64_t away = (int64_t)(b.first() - a.first());
+  if (a.ld != b.ld || a.es != b.es || away % a.es) return true;
+  if (away == 0) return !itself;
+  const int64_t off = ((away / a.es) % a.ld + a.ld) % a.ld;      // columns that b's rows begin behind a's
+  return !(off >= a.cols && a.ld - off >= b.cols);
 }
-// an output that may be its input, row on row, but not lie across it
-static bool lies_across(const Span& in, const Span& out, bool same_rows) {
-  if (out.first >= in.last || in.first >= out.last) return false;
-  return !(same_rows && in.first == out.first);
-}
+constexpr int kMaxVocab = 1 << 27;      // offsets inside a row, and a grid's second dimension
 static int element_size(int dtype) { return dtype == 1 ? 2 : 4; }
 static bool element_aligned(int dtype, const void* p) { return ((uintptr_t)p & (element_size(dtype) - 1)) == 0; }
 
@@ -253,7 +262,7 @@ int bk_rotary(int dtype, int T, int seq, int heads, int d, int rot, int interlea
   const int64_t cols = (int64_t)heads * d;
   if (cols > 0x7fffffff / 8 || ldx < cols || ldy < cols || !element_aligned(dtype, x) || !element_aligned(dtype, y)) return BAMBOO_E_ARG;
   const int es = element_size(dtype);
-  if (lies_across(span_of(x, T, ldx, cols, es), span_of(y, T, ldy, cols, es), ldx == ldy)) return BAMBOO_E_ARG;
+  if (overlap({x, T, ldx, cols, es}, {y, T, ldy, cols, es}, true)) return BAMBOO_E_ARG;
   RotaryDesc a;
   memset(&a, 0, sizeof(a));
   a.x = x; a.y = y; a.ldx = ldx; a.ldy = ldy; a.T = T; a.seq = seq; a.heads = heads; a.d = d; a.rot = rot;
@@ -302,6 +311,12 @@ static int cross_desc(CrossDesc& a, int dtype, int impl, int batch, int sq, int 
   a.ctx = (void*)ctx; a.ldc = ldc; a.lse = (float*)lse; a.scratch = scratch;
   return BAMBOO_OK;
 }
+static Matrix query_rows(const CrossDesc& a, int dtype, const void* p, int64_t ld) {
+  return {p, (int64_t)a.B * a.sq, ld, (int64_t)a.heads * a.d, element_size(dtype)};
+}
+static Matrix key_rows(const CrossDesc& a, int dtype, const void* p, int64_t ld) {
+  return {p, (int64_t)a.B * a.sk, ld, (int64_t)a.kv_heads * a.d, element_size(dtype)};
+}
 
 uint64_t bk_cross_attention_scratch_floats(int batch, int sq, int sk, int heads, int kv_heads, int d) {
   if (batch <= 0 || sq <= 0 || sk <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || d <= 0 || d > 128) return 0;
@@ -314,6 +329,9 @@ int bk_cross_attention_fwd(int dtype, int impl, int batch, int sq, int sk, int h
   CrossDesc a;
   const int rc = cross_desc(a, dtype, impl, batch, sq, sk, heads, kv_heads, d, q, ldq, k, v, ldkv, kv_len, ctx, ldc, lse, scratch);
   if (rc != BAMBOO_OK) return rc;
+  const Matrix out = query_rows(a, dtype, ctx, ldc);
+  if (overlap(query_rows(a, dtype, q, ldq), out) || overlap(key_rows(a, dtype, k, ldkv), out) || overlap(key_rows(a, dtype, v, ldkv), out))
+    return BAMBOO_E_ARG;
   (void)hipGetLastError();
   return finish(launch_cross_attention_fwd((hipStream_t)stream, dtype, impl, a));
 }
@@ -329,6 +347,13 @@ int bk_cross_attention_bwd(int dtype, int impl, int batch, int sq, int sk, int h
     return BAMBOO_E_ARG;
   for (const void* p : {dctx, (const void*)dq, (const void*)dk, (const void*)dv})
     if (!element_aligned(dtype, p)) return BAMBOO_E_ARG;
+  const Matrix in[] = {query_rows(a, dtype, q, ldq), query_rows(a, dtype, ctx, ldc), query_rows(a, dtype, dctx, lddc),
+                       key_rows(a, dtype, k, ldkv), key_rows(a, dtype, v, ldkv)};
+  const Matrix out[] = {query_rows(a, dtype, dq, lddq), key_rows(a, dtype, dk, lddkv), key_rows(a, dtype, dv, lddkv)};
+  for (const Matrix& o : out)
+    for (const Matrix& i : in)
+      if (overlap(i, o)) return BAMBOO_E_ARG;
+  if (overlap(out[0], out[1]) || overlap(out[0], out[2]) || overlap(out[1], out[2])) return BAMBOO_E_ARG;
   a.dctx = dctx; a.lddc = lddc; a.dq = dq; a.lddq = lddq; a.dk = dk; a.dv = dv; a.lddkv = lddkv;
   (void)hipGetLastError();
   return finish(launch_cross_attention_bwd((hipStream_t)stream, dtype, impl, a));
@@ -337,15 +362,14 @@ int bk_cross_attention_bwd(int dtype, int impl, int batch, int sq, int sk, int h
 // the gradient's buffer: whole elements, and either the logits' own rows or none of them
 static bool bad_gradient(int dtype, int64_t rows, int V, const void* logits, int64_t ldl, const void* dlogits, int64_t ldd) {
   const int es = element_size(dtype);
-  return ldd < V || !element_aligned(dtype, dlogits) ||
-         lies_across(span_of(logits, rows, ldl, V, es), span_of(dlogits, rows, ldd, V, es), ldl == ldd);
+  return ldd < V || !element_aligned(dtype, dlogits) || overlap({logits, rows, ldl, V, es}, {dlogits, rows, ldd, V, es}, true);
 }
 
 int bk_policy_loss(int dtype, int T, int V, const void* logits, int64_t ldl, const int32_t* labels, const uint8_t* mask,
                    const float* old_logp, const float* ref_logp, const float* adv, float clip_low, float clip_high,
                    float kl_coef, float ent_coef, float scale, float* logp, float* loss_tok, float* kl_tok,
                    float* entropy, void* dlogits, int64_t ldd, void* stream) {
-  if ((dtype != 0 && dtype != 1) || T <= 0 || V <= 0 || V > 0x7fff0000 || ldl < V) return BAMBOO_E_ARG;
+  if ((dtype != 0 && dtype != 1) || T <= 0 || V <= 0 || V > kMaxVocab || ldl < V) return BAMBOO_E_ARG;
   if (!logits || !labels || !old_logp || !adv || !logp || !loss_tok || !element_aligned(dtype, logits)) return BAMBOO_E_ARG;
   if (!(clip_low >= 0.f && clip_low <= 1.f && clip_high >= 0.f)) return BAMBOO_E_ARG;
   if (dlogits && bad_gradient(dtype, T, V, logits, ldl, dlogits, ldd)) return BAMBOO_E_ARG;
@@ -360,7 +384,7 @@ int bk_policy_loss(int dtype, int T, int V, const void* logits, int64_t ldl, con
 
 static int preference_desc(PreferenceDesc& a, int dtype, int pairs, int seq, int V, const void* logits, int64_t ldl,
                            const int32_t* labels, const uint8_t* mask, float beta, float smoothing) {
-  if ((dtype != 0 && dtype != 1) || pairs <= 0 || seq <= 0 || V <= 0 || V > 0x7fff0000 || ldl < V) return BAMBOO_E_ARG;
+  if ((dtype != 0 && dtype != 1) || pairs <= 0 || seq <= 0 || V <= 0 || V > kMaxVocab || ldl < V) return BAMBOO_E_ARG;
   if ((int64_t)2 * pairs * seq > 0x7fffffff || !logits || !labels || !element_aligned(dtype, logits)) return BAMBOO_E_ARG;
   if (!(smoothing >= 0.f && smoothing <= 1.f)) return BAMBOO_E_ARG;
   memset(&a, 0, sizeof(a));

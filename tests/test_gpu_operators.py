@@ -500,6 +500,70 @@ def test_adamw_gradients_that_are_not_finite_stay_in_their_place(B):
         assert bad == [300], bad
 
 
+# ---- rows far apart, two calls at once --------------------------------------------------------------------
+
+def test_rows_more_than_32_bits_apart(B):
+    """views of one buffer of 6.6 GB: offsets pass 2^32 bytes and 2^31 elements"""
+    wide = 1_100_000_000
+    buf = torch.empty(3, wide, dtype=torch.bfloat16, device=DEV)
+    rng = np.random.default_rng(0)
+    z, zd = draw(rng, (3, 1000), 1, 2.0)
+    buf[:, :1000] = zd
+    labels = np.array([1, 999, 500])
+    lab = torch.from_numpy(labels.astype(np.int32)).to(DEV)
+    one, logp, loss = torch.ones(3, device=DEV), torch.empty(3, device=DEV), torch.empty(3, device=DEV)
+    B.bk_policy_loss(buf[:, :1000], lab, -one, one, logp, loss, buf[:, 2000:3000])
+    want = O.policy_loss(z, labels, -np.ones(3), np.ones(3))
+    assert np.all(np.abs(host(buf[:, 2000:3000]) - want[4]) <= unit(1) * np.abs(want[4]) + 1e-5)
+    freq, _ = B.bk_rotary_frequencies(64)
+    x, xd = draw(rng, (3, 128), 1)
+    buf[:, 4000:4128] = xd
+    B.bk_rotary(buf[:, 4000:4128], freq, buf[:, 5000:5128], 2, 64, seq=3)
+    turned = O.rotary(x, O.rotary_frequencies(64)[0], np.arange(3), 2, 64)
+    within(buf[:, 5000:5128], turned, unit(1) * np.abs(turned) + 1e-5, "rotary")
+    # the same memory as 60000 keys of one head, 110 KB apart
+    rows = buf.view(-1)[:60000 * 55000].view(60000, 55000)
+    rows[:, :128] = torch.randn(60000, 128, device=DEV).bfloat16()
+    k, v = rows[:, :64], rows[:, 64:128]
+    q, g = torch.randn(4, 64, device=DEV).bfloat16(), torch.randn(4, 64, device=DEV).bfloat16()
+    ctx, dq, lse = torch.empty_like(q), torch.empty_like(q), torch.empty(1, 1, 4, device=DEV)
+    dk, dv = torch.empty(60000, 64, dtype=torch.bfloat16, device=DEV), torch.empty(60000, 64, dtype=torch.bfloat16, device=DEV)
+    B.bk_cross_attention_fwd(q, k, v, ctx, lse, 1, 1)
+    B.bk_cross_attention_bwd(q, k, v, ctx, lse, g, dq, dk, dv, 1, 1)
+    a = [host(t) for t in (q, k, v, g)]
+    want_ctx, want_lse = O.cross_attention_fwd(*a[:3], 1, 1, 1)
+    grads = O.cross_attention_bwd(*a, 1, 1, 1)
+    bounds = attention_bounds(*a, want_ctx, want_lse, 1, 1, 1, None, unit(1), unit(1))
+    for got, w, b in zip((ctx, lse, dq, dk, dv), (want_ctx, want_lse) + grads, bounds):
+        within(got, w, b + unit(1) * np.abs(w), "far")
+
+
+def test_calls_at_once_on_two_streams(B):
+    """each call has scratch of its own: two that overlap give what each gives alone"""
+    cases = [run_inputs(k) for k in (1, 2)]
+
+    def run(c, stream=None):
+        q, k, v, g, n = c
+        ctx, dq, dk, dv, lse = (torch.empty_like(t) for t in (q, q, k, v, torch.empty(4, 4, 1, device=DEV)))
+        B.bk_cross_attention_fwd(q, k, v, ctx, lse, 4, 4, 2, kv_len=n, stream=stream)
+        B.bk_cross_attention_bwd(q, k, v, ctx, lse, g, dq, dk, dv, 4, 4, 2, kv_len=n, stream=stream)
+        return ctx, lse, dq, dk, dv
+    alone = [run(c) for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(3):
+        got = [run(c, s) for c, s in zip(cases, streams)]
+        torch.cuda.synchronize()
+        for x, y in zip(alone, got):
+            assert all(torch.equal(a, b) for a, b in zip(x, y))
+
+
+def run_inputs(seed):
+    rng = np.random.default_rng(seed)
+    mk = lambda *s: draw(rng, s, 1)[1]
+    return mk(4, 256), mk(4 * 3000, 128), mk(4 * 3000, 128), mk(4, 256), torch.tensor([3000, 0, 1, 2999], dtype=torch.int32, device=DEV)
+
+
 # ---- graphs, streams, one step of them all --------------------------------------------------------------
 
 def test_captured_and_replayed(B):
