@@ -111,22 +111,30 @@ hipError_t join_bwd(hipStream_t s, int dtype, const CrossDesc& a) {
 
 long up4(long n) { return (n + 3) / 4 * 4; }
 
-// Parts of the streamed side (`streamed` rows) for `owned` rows of each of `pairs` problems: as many as `slots` workgroups
-// allow, of `least` tiles at least; two workgroups a CU in bf16, where each hides the other's waits, and one in fp32, whose
-// four wavefronts keep the matrix cores busy (with five parts of 64 workgroups in the place of four the CUs that got two of
-// them took 27 us, the others half).  A part's results (`floats`) are written and read again, 8 bytes each at 5 TB/s, so
-// that more than sqrt(time of all tiles / that) parts cost more than they save.  `tile_us`: a tile of 64 rows.  dK and dV of
-// 1 x 2048 x 4096, 96 heads over 8 of 128 (256 workgroups): 1018 us as one part, 830 + 28 as two; of 8 x 512 x 333, 16 heads
-// of 64 (384 workgroups): 26 us as one, 35 + 20 as two.
-int parts(long owned, long streamed, long pairs, long floats, float tile_us, int slots, int least) {
+// Parts of the streamed side (`streamed` rows) for `owned` rows of each of `pairs` problems: the number, of `least` tiles each
+// at least, with the smallest time by this account.  The busiest CU gets `k` workgroups.  In bf16 two of them at a time take
+// 1.6 times as long as one, each hiding the other's waits; in fp32 the four wavefronts of one keep the matrix cores busy and
+// the time is k times one's.  A tile of 64 rows takes a workgroup `tile_us`.  Joining is a launch, and a part's results
+// (`floats`) are written and read again at 5 TB/s.  Measured: dK and dV of 1 x 2048 x 4096, 96 heads over 8 of 128 (256
+// workgroups), 1018 us as one part, 830 + 28 as two; of 8 x 512 x 333, 16 heads of 64 (384), 26 us as one, 35 + 20 as two; in
+// fp32, 13 x 502 x 514, 32 heads over 4 of 128 (260, four more than CUs), 2231 us as one, 1350 + 40 as five.
+int parts(long owned, long streamed, long pairs, long floats, float tile_us, bool mfma, int least) {
   const long wgs = (owned + 127) / 128 * pairs, tiles = (streamed + 63) / 64;
-  long n = slots / wgs;
-  if (n > tiles / least) n = tiles / least;
-  const float most = sqrtf(tiles * tile_us / (floats * 1.6e-6f));
-  if (n > most) n = (long)most;
-  if (n <= 1) return 1;
-  const long per = (tiles + n - 1) / n;
-  return (int)((tiles + per - 1) / per);
+  const int most = (int)(tiles / least < 64 ? tiles / least : 64);
+  int best = 1;
+  float best_us = 0.f;
+  for (int n = 1; n <= most || n == 1; ++n) {
+    const long per = (tiles + n - 1) / n;
+    if (n > 1 && (tiles + per - 1) / per != n) continue;      // the last part would be empty
+    const long k = (wgs * n + 255) / 256;
+    const float units = mfma ? 1.6f * (k / 2) + (k & 1) : (float)k;
+    const float us = units * per * tile_us + (n > 1 ? 4.f + n * floats * 1.6e-6f : 0.f);
+    if (n == 1 || us < best_us) {
+      best = n;
+      best_us = us;
+    }
+  }
+  return best;
 }
 
 struct Plan {
@@ -137,11 +145,11 @@ Plan plan(bool mfma, int B, int sq, int sk, int heads, int kv_heads, int d) {
   const long pairs = (long)B * kv_heads, rows = (long)sq * (heads / kv_heads);
   const long row_floats = pairs * rows * d, key_floats = 2 * pairs * (long)sk * d;
   const float tile_us = mfma ? 0.4f + 0.008f * d : 0.5f + 0.05f * d;
-  const int slots = mfma ? 512 : 256, least = mfma ? 4 : 1;
+  const int least = mfma ? 4 : 1;
   Plan p;
-  p.fwd = parts(rows, sk, pairs, row_floats, tile_us, slots, least);
-  p.dq = parts(rows, sk, pairs, row_floats, 1.5f * tile_us, slots, least);
-  p.dkv = parts(sk, rows, pairs, key_floats, 2.f * tile_us, slots, least);
+  p.fwd = parts(rows, sk, pairs, row_floats, tile_us, mfma, least);
+  p.dq = parts(rows, sk, pairs, row_floats, 1.5f * tile_us, mfma, least);
+  p.dkv = parts(sk, rows, pairs, key_floats, 2.f * tile_us, mfma, least);
   p.fwd_floats = p.fwd > 1 ? up4(p.fwd * row_floats) + up4(p.fwd * pairs * rows * 2) : 0;
   p.delta = up4(pairs * rows);
   p.dq_floats = p.dq > 1 ? p.dq * up4(row_floats) : 0;

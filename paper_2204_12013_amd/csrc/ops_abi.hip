@@ -302,7 +302,7 @@ static int cross_desc(CrossDesc& a, int dtype, int impl, int batch, int sq, int 
   const int64_t group = heads / kv_heads, rows = sq * group, pairs = (int64_t)batch * kv_heads;
   const int64_t most = rows > sk ? rows : sk;
   if (rows > 0x7fffff00 || rows * group > 0xffffffffLL || sk > 0x7fffff00 || pairs > 0x7fffffff ||
-      (most / 4 + 1024) * pairs > 0x7fffffff || pairs * most * 2 * d / 256 + 1 > 0x7fffffff)
+      (most + 1024) * pairs > 0x7fffffff || pairs * most * 2 * d / 256 + 1 > 0x7fffffff)
     return BAMBOO_E_ARG;
   if ((!scratch && bk_cross_attention_scratch_floats(batch, sq, sk, heads, kv_heads, d) > 0) || ((uintptr_t)scratch & 15)) return BAMBOO_E_ARG;
   memset(&a, 0, sizeof(a));
