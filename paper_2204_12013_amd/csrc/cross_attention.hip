@@ -117,7 +117,7 @@ long up4(long n) { return (n + 3) / 4 * 4; }
 // the time is k times one's.  A tile of 64 rows takes a workgroup `tile_us`.  Joining is a launch, and a part's results
 // (`floats`) are written and read again at 5 TB/s.  Measured: dK and dV of 1 x 2048 x 4096, 96 heads over 8 of 128 (256
 // workgroups), 1018 us as one part, 830 + 28 as two; of 8 x 512 x 333, 16 heads of 64 (384), 26 us as one, 35 + 20 as two; in
-// fp32, 13 x 502 x 514, 32 heads over 4 of 128 (260, four more than CUs), 2231 us as one, 1350 + 40 as five.
+// fp32, 13 x 502 x 514, 32 heads over 4 of 128 (260, four more than CUs), 2231 us as one, 1351 + 57 as nine.
 int parts(long owned, long streamed, long pairs, long floats, float tile_us, bool mfma, int least) {
   const long wgs = (owned + 127) / 128 * pairs, tiles = (streamed + 63) / 64;
   const int most = (int)(tiles / least < 64 ? tiles / least : 64);
@@ -144,8 +144,9 @@ struct Plan {
 Plan plan(bool mfma, int B, int sq, int sk, int heads, int kv_heads, int d) {
   const long pairs = (long)B * kv_heads, rows = (long)sq * (heads / kv_heads);
   const long row_floats = pairs * rows * d, key_floats = 2 * pairs * (long)sk * d;
-  const float tile_us = mfma ? 0.4f + 0.008f * d : 0.5f + 0.05f * d;
-  const int least = mfma ? 4 : 1;
+  const bool padded = d != 64 && d != 128;          // tiles through registers
+  const float tile_us = mfma ? (0.4f + 0.008f * d) * (padded ? 1.6f : 1.f) : 0.5f + 0.05f * d;
+  const int least = mfma ? 2 : 1;
   Plan p;
   p.fwd = parts(rows, sk, pairs, row_floats, tile_us, mfma, least);
   p.dq = parts(rows, sk, pairs, row_floats, 1.5f * tile_us, mfma, least);

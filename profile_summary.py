@@ -14,10 +14,10 @@ import sys
 
 
 def _short(name):
-    name = name.replace("void ", "").replace("bamboo::", "")
+    name = name.replace("void ", "").replace("bamboo::", "").replace("(anonymous namespace)::", "")
     if name.startswith("_ZN6bamboo"):
         import re
-        m = re.match(r"_ZN6bamboo(\d+)", name)
+        m = re.match(r"_ZN6bamboo(?:12_GLOBAL__N_1)?(\d+)", name)
         n = int(m.group(1))
         name = name[len(m.group(0)):][:n] + "<...>"
     return name[:78]
