@@ -6,12 +6,14 @@
 // HBM-bound: per parameter 28 bytes of gradient, master weight and moments and the storage copy, or 16 + 1/16 with
 // moments in 8 bits.  One launch takes up to kAdamwTensors tensors, whose descriptors travel in the kernel's arguments
 // (nothing on the device has to outlive the call, and a captured graph holds its own copy); a workgroup finds its tensor
-// with one load per lane and a ballot.
+// with one load per lane and a ballot.  75.6 M parameters in 72 tensors: 386 us, 5.9 TB/s (two groups of 256 a wavefront 427 us,
+// storage weights kept in the caches 402 us); 184 M with moments in 8 bits: 595 us, 5.6 TB/s (codes made by comparisons and shifts
+// 658 us: the arithmetic was as long as the traffic).
 //
 // 8 bits: blocks of 256 elements share a scale (largest / 448) and each element is an e4m3 code, value = code * scale.
 // The second moment is held as its root: the codes span a factor of 2^17.8, so its own range is squared.  A wavefront owns
-// a block, four elements a lane.  Moments move by a tenth or a thousandth of themselves a step, less than half the
-// distance to the next code (1/16 to 1/32), so rounding to the nearest would keep them where they are for good; they
+// a block, four elements a lane.  The second moment moves by a thousandth of its way a step, less than half the distance
+// to the next code (1/16 to 1/32 of the value), so rounding to the nearest would keep it where it is for good; both
 // go up or down with the probability that keeps the mean, by 16 bits of a hash of (seed, step, tensor, element): the
 // same bits wherever the step runs.  A root that is not zero never becomes zero, which would make the next step huge.
 // The step itself uses the moments before they are rounded.

@@ -1,5 +1,5 @@
-// Attention over an encoder's states in fp32 arithmetic on the matrix cores, for fp32 and for the bf16 shapes that the
-// bf16 kernels do not take: any head size up to 128, any alignment.
+// Attention over an encoder's states in fp32 arithmetic on the matrix cores: fp32 tensors, and bf16 ones where a caller asks
+// for it; any head size up to 128, any alignment.
 //
 // Four wavefronts own 32 rows each and share tiles of 32 streamed rows, held in LDS in fp32 with the head size padded
 // by zeros to DP.  The score tile is computed transposed (streamed rows along a lane's registers, owned rows along the
@@ -7,7 +7,9 @@
 // accumulator is at once the operand of the second product: the streamed rows of its two halves are 8 (r / 4) + r % 4 and
 // that plus 4, and the other operand is read for just these.  The contraction over the head size runs over feature i of
 // the lower and DP / 2 + i of the upper half in step i, so that a lane's values are neighbours in LDS.
-// Bound by the matrix instruction: 64 clocks for 4096 multiply-adds, a sixteenth of the bf16 one's rate.
+// Bound by the matrix instruction: 64 clocks for 2048 multiply-adds, a sixteenth of the bf16 one's rate (a large library
+// product reaches 154 TFLOP/s).  13 x 502 x 514, 32 heads over 4 of 128: forward 518 us (106 TFLOP/s), dQ 850 us (97), dK and dV
+// 1351 us (81), one wavefront a SIMD in the backward; what is missing are the steps' own chains: barrier, scores, exponentials.
 #include <math.h>
 
 #include "cross_rows.h"

@@ -8,7 +8,10 @@
 // Bound by the traffic of the logits: the policy loss reads them once and writes the gradient once, which takes the row
 // on chip.  It is held in registers, in the storage type: a workgroup of 256 to 1024 threads requests its whole row at
 // once (up to 16 vectors of 16 bytes a thread), which also is what keeps enough loads in flight.  Rows beyond that are
-// read again.  All sums are in 32 bits, in a fixed order.
+// read again.  All sums are in 32 bits, in a fixed order; those over a sequence in 64.
+// 4096 x 50304 bf16 with KL and entropy, a quarter of the tokens left out (721 MB): 136 us, 5.3 TB/s (191 us with three
+// operations to an exponent, comparisons with the label, and 1024 threads a row, of which a CU holds one workgroup).  Preference
+// loss 4096 x 30528 bf16, half of the tokens left out: log-probabilities 23 us, gradient 50 us.
 #include <math.h>
 
 #include <type_traits>

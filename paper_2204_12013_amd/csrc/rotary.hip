@@ -3,7 +3,9 @@
 // pairs being (i, i + rot/2) or neighbours (2i, 2i + 1).  The backward turns the other way (the map is a rotation
 // times a number, so its transpose is the inverse rotation times that number).
 //
-// HBM-bound: every rotated element is read and written once.  A workgroup takes a few tokens and a range of heads;
+// HBM-bound: every rotated element is read and written once (2048 tokens, 192 heads of 128, half of each rotated and half
+// passed on, 201 MB: 44 us, 4.6 TB/s, as with other numbers of items in flight, heads to a workgroup and loops; with stores that
+// bypass the caches 42 us, but the next call reads what is stored here).  A workgroup takes a few tokens and a range of heads;
 // the angles' cosines and sines are formed once per token and pair, into LDS, and shared by all heads.
 // Angles are products in 64 bits, reduced to one turn there: at position 10^6 a 32-bit product would be off by up to
 // 0.03 rad.  The reduced angle, at most pi, is then exact to 2^-24 * pi in 32 bits.
