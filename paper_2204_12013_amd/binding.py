@@ -663,13 +663,14 @@ def _launch(fn, where, dev, stream, *args):
 
 
 def _scratch(n, dev, stream, where):
-    """n floats of scratch for one call, held by the allocator until the call's stream is through with it."""
+    """n floats of scratch for one call, from the allocator's pool of the call's own stream: what had the memory before ran
+    there, and what gets it next does."""
     if dev < 0:
         _refuse(where)
-    t = torch.empty(n, dtype=torch.float32, device=dev)
-    if stream is not None and stream.cuda_stream != _raw_stream(dev):
-        t.record_stream(stream)
-    return t
+    if stream is None:
+        return torch.empty(n, dtype=torch.float32, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(n, dtype=torch.float32, device=dev)
 
 
 ROTARY_SCALINGS = ("none", "linear", "stretched", "parts")
