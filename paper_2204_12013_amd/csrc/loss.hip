@@ -306,13 +306,14 @@ __global__ __launch_bounds__(NT) void policy_loss_kernel(PolicyDesc a) {
   const float old = a.old_logp[t], adv = a.adv[t], ref = a.ref_logp != nullptr ? a.ref_logp[t] : 0.f;
   RowPass<T, NT, NC, ENT> pass;
   const RowStats r = pass.run(row, a.V, label, red);
-  const float ratio = expf(r.logp - old);
+  // differences to logp from its parts: logp itself is rounded to a few 10^-7, which a small KL term would not forgive
+  const float below = r.at_label - r.top, ratio = expf((below - old) - r.log_s);
   const float free = ratio * adv, held = fminf(fmaxf(ratio, 1.f - a.clip_low), 1.f + a.clip_high) * adv;
   // the smaller of the two counts; a ratio or advantage that is NaN stays one
   const bool counts = !(free > held);
   float loss = -(counts ? free : held), coef = counts ? -free : 0.f, kl = 0.f;
   if (a.ref_logp != nullptr) {
-    const float away = ref - r.logp, grown = expm1f(away);
+    const float away = (ref - below) + r.log_s, grown = expm1f(away);
     kl = grown - away;
     loss = fmaf(a.kl_coef, kl, loss);
     coef = fmaf(-a.kl_coef, grown, coef);
