@@ -194,11 +194,12 @@ struct RowPass {
     r.entropy = ENT ? l - kLn2 * w / s : 0.f;
     return r;
   }
-  // of element j of a chunk: the exponent, and e_v
+  // of element j of a chunk: the exponent, and e_v.  Where e_v is what is held, an exponent below -126 has left 0: any finite one
+  // will do in its place, and the logarithm's -inf would not, 0 * -inf being NaN
   __device__ __forceinline__ static void term(const vec& v, int j, const RowStats& r, float* t, float* e) {
     if constexpr (KEEPS_EXP) {
       *e = v[j];
-      *t = __builtin_amdgcn_logf(*e);
+      *t = fmaxf(__builtin_amdgcn_logf(*e), kFar);
     } else {
       *t = fmaf(to_f32<T>(v[j]), kL2e, -r.m2);
       *e = __builtin_amdgcn_exp2f(*t);

@@ -1,0 +1,109 @@
+"""Operators around the stage where their inputs are unusual, and in the forms that large batches run (GPU only), against the
+64-bit oracle with derived bounds.  Units as in test_gpu_operators: u half a step of the storage type, E that of fp32."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import operators as O
+from paper_2204_12013_amd import synth
+from test_gpu_operators import B, DEV, E, f32, host, unit, within  # noqa: F401  (B is a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- losses ---------------------------------------------------------------------------------------
+
+def stored(z, dtype):
+    """the values that the storage type holds, as float64"""
+    return synth.round_to_storage(np.asarray(z, np.float32), dtype).astype(np.float64)
+
+
+def row_bounds(z, labels):
+    """(log-probabilities, error of a label's, relative error of a probability, per row and element)"""
+    at = np.arange(len(z))
+    t = z.max(1, keepdims=True) - z
+    lp = O.log_softmax(z)
+    p = np.exp(lp)
+    t0 = np.where(p > 0, t, 0.0)
+    # exponents: two roundings of t log2 e each; sums of at most 128 terms a thread (V / 1024 of longer rows), then 22 more.  The
+    # maximum itself cancels: logits enter as differences to it, and what its own product is rounded by is taken back
+    s = E * (4 * (p * t0).sum(1) + max(128, z.shape[1] / 512) + 30)
+    b = s + E * (8 + t[at, labels] + 2 * np.abs(np.log(np.exp(-t).sum(1))))
+    return lp, b, E * 4 * (t0 + 2) + b[:, None]
+
+
+def check_policy(B, z, labels, dtype, T=None, extra=0, ent=0.01, with_ref=True, scale=0.25):
+    """the rows of z among T rows of which no other counts: all outputs"""
+    n, V = z.shape
+    T = n if T is None else T
+    rng = np.random.default_rng(V)
+    z = stored(z, dtype)
+    rows = np.sort(rng.permutation(T)[:n])
+    act = torch.bfloat16 if dtype == 1 else torch.float32
+    logits = torch.full((T, V + extra), float("nan"), dtype=act, device=DEV)[:, :V]
+    logits[torch.from_numpy(rows).to(DEV)] = torch.from_numpy(z).to(DEV).to(act)
+    lp, b, rel = row_bounds(z, labels)
+    p, at = np.exp(lp), np.arange(n)
+    now = lp[at, labels]
+    old, ref = (np.float32(now + k * rng.normal(size=n)).astype(np.float64) for k in (0.2, 0.4))
+    adv = np.float32(rng.normal(size=n)).astype(np.float64)
+    kw = dict(clip_low=0.2, clip_high=0.3, kl_coef=0.1, ent_coef=ent, scale=scale)
+    c32 = {k: float(np.float32(v)) for k, v in kw.items()}
+    want = O.policy_loss(z, labels, old, adv, ref if with_ref else None, None, **c32)
+
+    def spread(x, dtype=torch.float32):
+        t = torch.full((T,), 3, dtype=dtype, device=DEV)
+        t[torch.from_numpy(rows).to(DEV)] = torch.from_numpy(np.asarray(x)).to(DEV).to(dtype)
+        return t
+    mask = torch.zeros(T, dtype=torch.uint8, device=DEV)
+    mask[torch.from_numpy(rows).to(DEV)] = 1
+    logp, loss, kl, entropy = (torch.full((T,), 9.0, device=DEV) for _ in range(4))
+    whole = torch.full((T, V + extra), 5.0, dtype=act, device=DEV)
+    d = whole[:, :V]
+    args = (spread(labels, torch.int32), spread(old), spread(adv), logp, loss)
+    keep = dict(mask=mask, ref_logp=spread(ref) if with_ref else None, kl_tok=kl, entropy=entropy, **kw)
+    B.bk_policy_loss(logits, *args, d, **keep)
+    lp0 = np.where(p > 0, lp, 0.0)
+    r = np.exp(now - old)
+    grow = np.exp(ref - now) if with_ref else 0.0
+    b_ent = b + (p * (np.abs(lp0) + 1) * rel).sum(1) + E * 200 * (p * np.abs(lp0)).sum(1)
+    b_kl = (b + 4 * E) * np.abs(grow - 1) + 4 * E * (grow + np.abs(now) + 1) * with_ref
+    b_c = np.abs(r * adv) * (b + 8 * E * (1 + np.abs(now))) + c32["kl_coef"] * (b_kl + grow * (b + 4 * E)) + 8 * E
+    got = lambda t: host(t)[rows]
+    within(got(logp), want[0], b, "logp")
+    within(got(entropy), want[3], b_ent, "entropy")
+    within(got(kl), want[2], b_kl, "kl")
+    within(got(loss), want[1], b_c + c32["kl_coef"] * b_kl + ent * b_ent + 8 * E * np.abs(want[1]), "loss")
+    c = np.abs(r * adv) + c32["kl_coef"] * np.abs(grow - 1)
+    hit = np.zeros(z.shape)
+    hit[at, labels] = 1
+    b_d = b_c[:, None] * (hit + p) + p * (rel + 8 * E) * (c[:, None] + ent * (np.abs(lp0) + want[3][:, None])) + \
+        ent * p * (b[:, None] + b_ent[:, None]) + hit * 4 * E * c[:, None]
+    chosen = d[torch.from_numpy(rows).to(DEV)]
+    within(chosen, want[4], c32["scale"] * b_d + unit(dtype) * np.abs(want[4]) + 1e-38, "dlogits")
+    left = torch.ones(T, dtype=torch.bool, device=DEV)
+    left[torch.from_numpy(rows).to(DEV)] = False
+    assert not bool(d[left].any()) and all(not bool(t[left].any()) for t in (logp, loss, kl, entropy))
+    assert not extra or bool((whole[:, V:] == 5).all())
+    B.bk_policy_loss(logits, *args, logits, **keep)                             # in place: the same bits
+    assert torch.equal(logits, d)
+
+
+def banned(V, values):
+    """six rows of logits with a share of them at `values`, and labels that may be chosen: one row's own is a low one"""
+    rng = np.random.default_rng(V)
+    z, labels = rng.standard_normal((6, V)) * 2.5, rng.integers(V // 2, V, 6)
+    for row in range(5):
+        z[row, :V // 2] = np.where(rng.random(V // 2) < 0.3, values[row % len(values)], z[row, :V // 2])
+    z[5, labels[5]] = -95.0
+    z[0, V - 1], labels[0] = values[0], V - 2
+    return z, labels
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("T", [6, 300])
+@pytest.mark.parametrize("V", [100, 300, 4096, 32000, 50304, 140001])
+@pytest.mark.parametrize("ent", [0.01, 0.0])
+def test_policy_loss_of_tokens_that_are_all_but_ruled_out(B, dtype, T, V, ent):
+    """logits so far below the row's maximum that their probability is 0 in 32 bits: all outputs finite and right"""
+    check_policy(B, *banned(V, [-95.0, -100.0, -1e4, -1e9, -1e30]), dtype, T=T, ent=ent)
