@@ -43,7 +43,7 @@ template <typename T> __device__ __forceinline__ typename Chunk<T>::type load_ch
   if (v + Chunk<T>::N <= V) return *(const typename Chunk<T>::loose*)(row + v);
   typename Chunk<T>::type x;
 #pragma unroll
-  for (int j = 0; j < Chunk<T>::N; ++j) x[j] = v + j < V ? row[v + j] : (T)(-INFINITY);    // adds nothing
+  for (int j = 0; j < Chunk<T>::N; ++j) x[j] = v + j < V ? row[v + j] : (T)(-INFINITY);    // no maximum, and adds nothing
   return x;
 }
 // STREAM: not to be kept in the caches.  Gradients that do not fit there any more would only push out the logits that are still
@@ -117,6 +117,7 @@ struct RowPass {
       for (int c = 0; c < NC; ++c)
         if (place(c) < V) x[c] = load_chunk<T>(row, place(c), V);
       centre(&r, block_max<NT>(own_max(V), red));
+      if constexpr (ENT) close(V);
 #pragma unroll
       for (int c = 0; c < NC; ++c)
         if (place(c) < V)
@@ -229,6 +230,18 @@ struct RowPass {
 #pragma unroll
         for (int j = 0; j < E; ++j) m = fmaxf(m, to_f32<T>(x[c][j]));
     return m;
+  }
+  // What fills the last vector behind the row's end has been -inf for the maximum; from here on it is far below it but finite, so
+  // that e * t is 0 there and `far` speaks of the row's own logits alone.
+  __device__ __forceinline__ void close(int V) {
+    const int chunk = V / E;                                      // the partial one, of thread chunk % NT
+    if (V % E == 0) return;
+#pragma unroll
+    for (int c = 0; c < HELD; ++c)
+      if (c == chunk / NT && (int)threadIdx.x == chunk % NT)
+#pragma unroll
+        for (int j = 0; j < E; ++j)
+          if (j >= V % E) x[c][j] = from_f32<T>(-1e30f);
   }
   __device__ __forceinline__ static void centre(RowStats* r, float top) {
     r->top = top == -INFINITY ? 0.f : top;

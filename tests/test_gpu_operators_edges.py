@@ -107,3 +107,10 @@ def banned(V, values):
 def test_policy_loss_of_tokens_that_are_all_but_ruled_out(B, dtype, T, V, ent):
     """logits so far below the row's maximum that their probability is 0 in 32 bits: all outputs finite and right"""
     check_policy(B, *banned(V, [-95.0, -100.0, -1e4, -1e9, -1e30]), dtype, T=T, ent=ent)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("V", [100, 300, 2051, 4096, 32003, 50257, 140001])
+def test_policy_loss_of_tokens_that_are_ruled_out(B, dtype, V):
+    """logits of -inf take no part, in vocabularies that fill their last vector and that do not"""
+    check_policy(B, *banned(V, [-np.inf]), dtype)
