@@ -190,7 +190,9 @@ int bk_policy_loss(int dtype, int T, int V, const void* logits, int64_t ldl, con
 int bk_preference_loss_fwd(int dtype, int pairs, int seq, int V, const void* logits, int64_t ldl, const int32_t* labels,
                            const uint8_t* mask, const float* ref_logp, float beta, float smoothing, float* lse,
                            float* logp, float* logp_seq, float* margin, float* loss, double* scratch, void* stream);
-/* dlogits[t,:] = scale * d loss[pair of t] / d logits[t,:]; dlogits may be logits (with ldd = ldl). */
+/* dlogits[t,:] = scale * d loss[pair of t] / d logits[t,:]; dlogits may be logits (with ldd = ldl).  Probabilities are
+ * exp(logits - lse): as fp32 holds lse, they are off by |lse| 2^-24 of themselves (a row whose logits all lie near -1e30 is not
+ * normalised any more). */
 int bk_preference_loss_bwd(int dtype, int pairs, int seq, int V, const void* logits, int64_t ldl, const int32_t* labels,
                            const uint8_t* mask, const float* lse, const float* margin, float beta, float smoothing,
                            float scale, void* dlogits, int64_t ldd, void* stream);

@@ -25,6 +25,7 @@ namespace {
 // exp(t) for t <= 0: the product with log2 e in two parts, whose rounding would otherwise shift every term the same way
 constexpr float kL2e = 1.4426950408889634f, kL2eRest = 1.9259629911266175e-8f, kLn2 = 0.6931471805599453f;
 constexpr float kFar = -300.f;      // an exponent of 2 whose power is 0
+constexpr float kWide = 1 << 20;    // maxima from here on are taken off the logits before anything else
 __device__ __forceinline__ float exp_of(float t) { return __builtin_amdgcn_exp2f(fmaf(t, kL2eRest, t * kL2e)); }
 
 // 16 bytes of a row, at any alignment of an element (the rows of a vocabulary that divides by nothing start anywhere)
@@ -91,9 +92,12 @@ __device__ __forceinline__ int clamp_label(int id, int V) { return id < 0 ? 0 : 
 
 // What a row's pass leaves.  e_v below is 2^(z_v log2 e - m2) with m2 = round(max log2 e), one multiply-add and the
 // exponential: what m2 is off by shifts all e_v and their sum alike, so that p_v = e_v / sum is free of it; from the sum's
-// logarithm it is taken back (`slip`).  (What log2 e is off by, 1e-8 of the distance to the maximum, stays.)
+// logarithm it is taken back (`slip`).  (What log2 e is off by, 1e-8 of the distance to the maximum, stays.)  From a maximum of
+// 2^20 on `slip` would grow beyond a sixteenth, and m2 out of the range of 32 bits in the end (a row that a mask has set to -1e30 or the
+// type's lowest value): there z_v - base with base = max stands in for z_v, in the storage type too: it is exact where z_v is
+// within a factor of two of the maximum, and so far away otherwise that e_v is 0.
 struct RowStats {
-  float top, m2;           // maximum (0 in the place of -inf)
+  float top, base, m2;     // maximum (0 in the place of -inf); the maximum from kWide on, otherwise 0; see above
   float sum, log_s, slip;  // of e_v; log of the sum of exp(z_v - top), = log(sum) - slip
   float at_label, logp, entropy;
   bool far;                // logits so far below the maximum that the distance is -inf
@@ -117,6 +121,13 @@ struct RowPass {
       for (int c = 0; c < NC; ++c)
         if (place(c) < V) x[c] = load_chunk<T>(row, place(c), V);
       centre(&r, block_max<NT>(own_max(V), red));
+      if (r.base != 0.f) {                                        // the same for the whole workgroup
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+          if (place(c) < V)
+#pragma unroll
+            for (int j = 0; j < E; ++j) x[c][j] = from_f32<T>(to_f32<T>(x[c][j]) - r.base);
+      }
       if constexpr (ENT) close(V);
 #pragma unroll
       for (int c = 0; c < NC; ++c)
@@ -202,7 +213,7 @@ struct RowPass {
       *e = v[j];
       *t = fmaxf(__builtin_amdgcn_logf(*e), kFar);
     } else {
-      *t = fmaf(to_f32<T>(v[j]), kL2e, -r.m2);
+      *t = fmaf(NC > 0 ? to_f32<T>(v[j]) : to_f32<T>(v[j]) - r.base, kL2e, -r.m2);
       *e = __builtin_amdgcn_exp2f(*t);
     }
   }
@@ -245,8 +256,10 @@ struct RowPass {
   }
   __device__ __forceinline__ static void centre(RowStats* r, float top) {
     r->top = top == -INFINITY ? 0.f : top;
-    r->m2 = r->top * kL2e;
-    r->slip = (fmaf(r->top, kL2e, -r->m2) + r->top * kL2eRest) * kLn2;
+    r->base = fabsf(r->top) >= kWide ? r->top : 0.f;
+    const float near = r->top - r->base;                          // NaN for +inf
+    r->m2 = near * kL2e;
+    r->slip = (fmaf(near, kL2e, -r->m2) + near * kL2eRest) * kLn2;
   }
 };
 

@@ -114,3 +114,41 @@ def test_policy_loss_of_tokens_that_are_all_but_ruled_out(B, dtype, T, V, ent):
 def test_policy_loss_of_tokens_that_are_ruled_out(B, dtype, V):
     """logits of -inf take no part, in vocabularies that fill their last vector and that do not"""
     check_policy(B, *banned(V, [-np.inf]), dtype)
+
+
+def level(V, dtype):
+    """six rows whose largest logits are far from 0, several of them alike, and labels among those"""
+    low = float(torch.finfo(torch.bfloat16 if dtype == 1 else torch.float32).min)
+    rng = np.random.default_rng(V)
+    z = np.tile(np.array([low, -1e30, -1e10, -3e6, 1e30, -2e30])[:, None], (1, V))
+    z[3] += rng.integers(0, 2, V) * (1 << 16)                          # two levels, both held exactly
+    z[4, :V // 2] = 0.0
+    z[5, V // 3:] = low
+    z[1, :V // 4] = -np.inf
+    return z, np.array([V - 1, V - 1, 0, int(z[3].argmax()), V - 1, 0])
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("T", [6, 300])
+@pytest.mark.parametrize("V", [100, 2051, 32000, 50304, 140001])
+def test_policy_loss_of_rows_far_from_zero(B, dtype, T, V):
+    """a row that a mask has set to the type's lowest value, or to another far one, throughout: the tokens are alike"""
+    check_policy(B, *level(V, dtype), dtype, T=T)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("pairs,V", [(3, 100), (300, 2051), (3, 140001)])
+def test_sequences_of_rows_far_from_zero(B, dtype, pairs, V):
+    z, labels = level(V, dtype)
+    z, n = stored(z, dtype), 2 * pairs
+    pick = np.arange(n) % 6
+    act = torch.bfloat16 if dtype == 1 else torch.float32
+    zd = torch.from_numpy(z).to(DEV).to(act)[torch.from_numpy(pick).to(DEV)]
+    lse, logp, seqs = (torch.empty(n, device=DEV) for _ in range(3))
+    margin, loss = torch.empty(pairs, device=DEV), torch.empty(pairs, device=DEV)
+    lp, b, _ = row_bounds(z, labels)
+    now, b = lp[np.arange(6), labels][pick], b[pick]
+    B.bk_preference_loss_fwd(zd, torch.from_numpy(labels[pick].astype(np.int32)).to(DEV), f32(np.zeros(n)), lse, logp, seqs, margin, loss, 0.5)
+    within(logp, now, b, "logp")
+    within(seqs, now, b, "sums")
+    within(margin, 0.5 * (now[:pairs] - now[pairs:]), b[:pairs] + b[pairs:], "margin")
