@@ -414,7 +414,9 @@ __global__ __launch_bounds__(256) void pair_loss_kernel(PreferenceDesc a) {
     a.logp_seq[i] = (float)c;
     a.logp_seq[a.pairs + i] = (float)r;
     a.margin[i] = (float)margin;
-    a.loss[i] = (float)((1. - (double)a.smoothing) * softplus(-margin) + (double)a.smoothing * softplus(margin));
+    // a side without weight adds nothing, infinite or not
+    const double yes = 1. - (double)a.smoothing, no = (double)a.smoothing;
+    a.loss[i] = (float)((yes > 0. ? yes * softplus(-margin) : 0.) + (no > 0. ? no * softplus(margin) : 0.));
   }
 }
 

@@ -152,3 +152,19 @@ def test_sequences_of_rows_far_from_zero(B, dtype, pairs, V):
     within(logp, now, b, "logp")
     within(seqs, now, b, "sums")
     within(margin, 0.5 * (now[:pairs] - now[pairs:]), b[:pairs] + b[pairs:], "margin")
+
+
+def test_preference_loss_of_a_sequence_that_cannot_be(B):
+    """a label of probability 0: the margin is infinite, and a side of the loss that has no weight adds nothing"""
+    pairs, V = 3, 50
+    z = torch.randn(2 * pairs, V, device=DEV)
+    lab = torch.full((2 * pairs,), 7, dtype=torch.int32, device=DEV)
+    z[3, 7] = z[1, 7] = -float("inf")                                           # rejected of pair 0, chosen of pair 1
+    for smoothing, want in ((0.0, [0.0, np.inf]), (1.0, [np.inf, 0.0]), (0.25, [np.inf, np.inf])):
+        lse, logp, seqs = (torch.empty(2 * pairs, device=DEV) for _ in range(3))
+        margin, loss, d = torch.empty(pairs, device=DEV), torch.empty(pairs, device=DEV), torch.empty_like(z)
+        B.bk_preference_loss_fwd(z, lab, torch.zeros(2 * pairs, device=DEV), lse, logp, seqs, margin, loss, 0.5, smoothing)
+        B.bk_preference_loss_bwd(z, lab, lse, margin, d, 0.5, smoothing)
+        assert margin[:2].tolist() == [np.inf, -np.inf]
+        assert loss[:2].tolist() == want and bool(loss[2].isfinite())
+        assert bool(d.isfinite().all())
