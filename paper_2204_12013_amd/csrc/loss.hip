@@ -420,7 +420,9 @@ __global__ __launch_bounds__(256) void pair_loss_kernel(PreferenceDesc a) {
   }
 }
 
-// dlogits = scale * dL/dlogp_seq * ([v = label] - p), dL/dlogp_seq = +-beta (sigmoid(margin) - (1 - smoothing)).
+// dlogits = scale * dL/dlogp_seq * ([v = label] - p), dL/dlogp_seq = +-beta (sigmoid(margin) - (1 - smoothing)), here as
+// smoothing sigmoid(margin) - (1 - smoothing) sigmoid(-margin): of pairs that are told apart well sigmoid(margin) is 1 to the last
+// bit, and the difference to 1 is all there is.
 // A workgroup takes four chunks a thread of a row: no thread needs another's, and the rows of a short batch fill the chip.
 constexpr int kAhead = 4;
 template <typename T, bool STREAM>
@@ -447,7 +449,8 @@ __global__ __launch_bounds__(256) void preference_bwd_kernel(PreferenceDesc a) {
   const int label = clamp_label(a.labels[t], a.V);
   const int seq = (int)(t / a.seq), pair = seq < a.pairs ? seq : seq - a.pairs;
   const float lse = a.lse[t];
-  const double g = 1. / (1. + exp(-(double)a.margin[pair])) - (1. - (double)a.smoothing);
+  const double m = a.margin[pair], e = exp(-fabs(m)), most = 1. / (1. + e), least = e * most;
+  const double g = (double)a.smoothing * (m >= 0. ? most : least) - (1. - (double)a.smoothing) * (m >= 0. ? least : most);
   const float coef = (float)((seq < a.pairs ? g : -g) * (double)a.beta * (double)a.scale);
 #pragma unroll
   for (int q = 0; q < kAhead; ++q) {

@@ -168,3 +168,26 @@ def test_preference_loss_of_a_sequence_that_cannot_be(B):
         assert margin[:2].tolist() == [np.inf, -np.inf]
         assert loss[:2].tolist() == want and bool(loss[2].isfinite())
         assert bool(d.isfinite().all())
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("smoothing", [0.0, 0.1, 1.0])
+def test_preference_gradient_of_pairs_that_are_told_apart_well(B, dtype, smoothing):
+    """margins at which a sigmoid is 1 to the last bit, and the gradient its difference to 1"""
+    rng = np.random.default_rng(5)
+    margins = np.array([60.0, -60.0, 35.0, -35.0, 18.0, -18.0, 0.25])
+    pairs, V = len(margins), 200
+    z = stored(rng.normal(size=(2 * pairs, V)), dtype)
+    labels = rng.integers(0, V, 2 * pairs)
+    zd = torch.from_numpy(z).to(DEV).to(torch.bfloat16 if dtype == 1 else torch.float32)
+    lp = O.log_softmax(z)
+    lse = f32(z[:, 0] - lp[:, 0])
+    d, sm = torch.empty_like(zd), float(np.float32(smoothing))
+    B.bk_preference_loss_bwd(zd, torch.from_numpy(labels.astype(np.int32)).to(DEV), lse, f32(margins), d, 0.5, smoothing)
+    g = 0.5 * (sm / (1 + np.exp(-margins)) - (1 - sm) / (1 + np.exp(margins)))
+    hit = np.zeros(z.shape)
+    hit[np.arange(2 * pairs), labels] = 1
+    c, p = np.concatenate([g, -g])[:, None], np.exp(lp)
+    # the coefficient rounded once, an exponential of a difference to a rounded lse, a product and a difference
+    bound = np.abs(c) * (E * hit + p * E * (8 + 4 * np.abs(lp) + 2 * np.abs(host(lse))[:, None]))
+    within(d, c * (hit - p), bound + (unit(dtype) + 2 * E) * np.abs(c * (hit - p)) + 1e-38, "dlogits")
