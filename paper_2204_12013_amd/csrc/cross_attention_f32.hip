@@ -335,6 +335,10 @@ __global__ __launch_bounds__(256, 1) void cross_dkv_f32_kernel(CrossDesc a) {
     add_product<DP>(dk, Qs, dp);
   }
   if (key >= a.sk) return;
+  if (!counts) {                                  // their probabilities are 0, but 0 times a row that is not finite is NaN
+    clear(dk);
+    clear(dv);
+  }
   if (a.splits > 1) {
     float* out = a.part + w.split * a.part_stride + ((long)w.pair * a.sk + key) * (2 * d);
     store_row<float, DP, VEC>(out, dk, 1.f, d);

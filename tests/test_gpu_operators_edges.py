@@ -191,3 +191,38 @@ def test_preference_gradient_of_pairs_that_are_told_apart_well(B, dtype, smoothi
     # the coefficient rounded once, an exponential of a difference to a rounded lse, a product and a difference
     bound = np.abs(c) * (E * hit + p * E * (8 + 4 * np.abs(lp) + 2 * np.abs(host(lse))[:, None]))
     within(d, c * (hit - p), bound + (unit(dtype) + 2 * E) * np.abs(c * (hit - p)) + 1e-38, "dlogits")
+
+
+# ---- attention over an encoder's states -------------------------------------------------------------
+
+@pytest.mark.parametrize("garbage", [float("nan"), float("inf")])
+@pytest.mark.parametrize("sq,heads,kv_heads,d", [(40, 4, 2, 64), (3000, 1, 1, 128), (9, 6, 2, 33)])
+@pytest.mark.parametrize("dtype,impl", [(0, 0), (1, 2), (1, 1)])
+def test_rows_that_are_not_finite_stay_among_what_they_meet(B, dtype, impl, sq, heads, kv_heads, d, garbage):
+    """a query or a gradient that is not finite: keys that do not count keep their zeros, other rows and samples their values"""
+    batch, sk, n = 3, 150, [70, 0, 129]
+    act = torch.bfloat16 if dtype == 1 else torch.float32
+    mk = lambda rows, cols: torch.randn(rows, cols, device=DEV).to(act)
+    q, k, v, g = mk(batch * sq, heads * d), mk(batch * sk, kv_heads * d), mk(batch * sk, kv_heads * d), mk(batch * sq, heads * d)
+    lens = torch.tensor(n, dtype=torch.int32, device=DEV)
+
+    def run(q, g):
+        ctx, dq, dk, dv, lse = (torch.full_like(t, 3.0) for t in (q, q, k, v, torch.empty(batch, heads, sq, device=DEV)))
+        B.bk_cross_attention_fwd(q, k, v, ctx, lse, batch, heads, kv_heads, kv_len=lens, impl=impl)
+        B.bk_cross_attention_bwd(q, k, v, ctx, lse, g, dq, dk, dv, batch, heads, kv_heads, kv_len=lens, impl=impl)
+        return ctx, dq, dk, dv
+    clean = run(q, g)
+    for which, sample in (("q", 0), ("g", 2), ("g", 0), ("q", 2)):
+        bad_q, bad_g = q.clone(), g.clone()
+        row = sample * sq + sq // 2
+        (bad_q if which == "q" else bad_g)[row, d // 2] = garbage
+        got = run(bad_q, bad_g)
+        for b in range(batch):
+            for t, c in zip(got[2:], clean[2:]):
+                rows = slice(b * sk + n[b], (b + 1) * sk)
+                assert not bool(t[rows].any()), (which, b)
+                if b != sample:
+                    assert torch.equal(t[b * sk:(b + 1) * sk], c[b * sk:(b + 1) * sk]), (which, b)
+        others = torch.arange(batch * sq, device=DEV) != row
+        for t, c in zip(got[:2], clean[:2]):
+            assert torch.equal(t[others], c[others]), which
