@@ -246,10 +246,11 @@ struct Matrix {
 static bool overlap(const Matrix& a, const Matrix& b, bool itself = false) {
   if (a.first() >= b.last() || b.first() >= a.last()) return false;
   const int64_t away = (int64_t)(b.first() - a.first());
-  if (a.ld != b.ld || a.es != b.es || away % a.es) return true;
+  const int64_t ld = a.rows == 1 ? b.ld : a.ld;                  // the distance between the rows of a single one says nothing
+  if ((ld != b.ld && b.rows > 1) || a.es != b.es || away % a.es) return true;
   if (away == 0) return !itself;
-  const int64_t off = ((away / a.es) % a.ld + a.ld) % a.ld;      // columns that b's rows begin behind a's
-  return !(off >= a.cols && a.ld - off >= b.cols);
+  const int64_t off = ((away / a.es) % ld + ld) % ld;            // columns that b's rows begin behind a's
+  return !(off >= a.cols && ld - off >= b.cols);
 }
 constexpr int kMaxVocab = 1 << 27;      // offsets inside a row, and a grid's second dimension
 static int element_size(int dtype) { return dtype == 1 ? 2 : 4; }

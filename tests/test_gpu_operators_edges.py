@@ -226,3 +226,20 @@ def test_rows_that_are_not_finite_stay_among_what_they_meet(B, dtype, impl, sq, 
         others = torch.arange(batch * sq, device=DEV) != row
         for t, c in zip(got[:2], clean[:2]):
             assert torch.equal(t[others], c[others]), which
+
+
+# ---- rotary positions -------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("T", [1, 2, 9])
+def test_rotary_in_place_through_a_narrower_view(B, dtype, T):
+    """queries and keys of a packed row written over themselves, the values beside them kept: one token as well as many"""
+    act = torch.bfloat16 if dtype == 1 else torch.float32
+    x = torch.randn(T, 3 * 2 * 64, device=DEV).to(act)
+    freq, _ = B.bk_rotary_frequencies(64)
+    pos = torch.arange(1000, 1000 + T, dtype=torch.int32, device=DEV)
+    want = torch.empty(T, 256, dtype=act, device=DEV)
+    B.bk_rotary(x, freq, want, 4, 64, pos=pos)
+    values = x[:, 256:].clone()
+    B.bk_rotary(x, freq, x[:, :256], 4, 64, pos=pos)
+    assert torch.equal(x[:, :256], want) and torch.equal(x[:, 256:], values)

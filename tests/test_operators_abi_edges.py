@@ -1,0 +1,20 @@
+"""More of what the operators' entry points take and refuse, on the host (no GPU: a call that got past its checks would try a launch
+and come back with another status than the one asked for)."""
+import pytest
+import torch
+
+from paper_2204_12013_amd import binding as B
+from test_operators_abi import CROSS_BWD, P, P2, POLICY, ROTARY
+
+
+def test_the_row_distance_of_a_single_row_says_nothing():
+    """one token through views of different widths: in place, and into columns beside each other"""
+    row, columns = dict(ROTARY, T=1, pos=P), dict(CROSS_BWD, batch=1, sq=1, sk=1, ldkv=256, v=P2 + 2 * 128)
+    assert B.lib.bk_rotary(*dict(row, y=P + 2, ldy=300).values()) == B.E_ARG
+    assert B.lib.bk_cross_attention_bwd(*dict(columns, dk=P2 + 2 * 64).values()) == B.E_ARG
+    assert B.lib.bk_cross_attention_bwd(*dict(columns, dq=P2 + 2 * 200, lddq=1000).values()) == B.E_ARG
+    if torch.cuda.is_available():
+        pytest.skip("the addresses are none: without a GPU the launch itself is what fails")
+    for change in (dict(ldx=300), dict(ldy=300), dict(ldx=128, ldy=1 << 33), dict(y=P + 2 * 128, ldy=300)):
+        assert B.lib.bk_rotary(*dict(row, **change).values()) == B.E_HIP
+    assert B.lib.bk_policy_loss(*dict(POLICY, T=1, ldd=200).values()) == B.E_HIP
