@@ -205,8 +205,8 @@ int bk_preference_loss_bwd(int dtype, int pairs, int seq, int V, const void* log
  * [ceil(numel/256)]: element i of m is code * m_scale[i/256], the ROOT of element i of v is code * v_scale[i/256]; all
  * zero bits are zero moments.  The step uses the moments before they are rounded to codes; the rounding goes up or down by
  * bits that depend on (seed, step, the tensor's place in the list, the element) alone, so that replicas that make the
- * same calls stay equal to the bit.  A gradient that is not finite makes its element's moments, an infinite one its whole
- * block's, NaN.  No two tensors may overlap.  Any alignment of an element; the fast form takes pointers aligned to 16
+ * same calls stay equal to the bit.  With 8 bits a gradient that is NaN makes its element's moments NaN, an infinite one its
+ * whole block's (and a finite one whose square is not, the block's second moments).  No two tensors may overlap.  Any alignment of an element; the fast form takes pointers aligned to 16
  * bytes (w and codes: to four elements). */
 int bk_adamw_group(int dtype, int moment_bits, int n, const int64_t* numel, const float* const* g, float* const* master,
                    void* const* m, void* const* v, float* const* m_scale, float* const* v_scale, void* const* w,

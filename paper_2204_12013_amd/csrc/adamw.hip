@@ -106,11 +106,14 @@ __host__ __device__ __forceinline__ unsigned mix(unsigned x) {
 
 // |x| inv, at most 448, moved to one of the two codes around it: up where the part beyond the lower one and `up` / 65536 (plus
 // half of that unit) make a whole step, codes being 2^(e-3) apart in [2^e, 2^(e+1)) and 2^-9 below 2^-6.  The conversion
-// adds 20 bits behind the code's last, of which these are the first 17; NaN stays NaN.
+// adds 20 bits behind the code's last, of which these are the first 17; NaN stays NaN, and so does an infinite x, whose block's
+// inv is 0.
 __device__ __forceinline__ float scaled(float x, float inv) {
   const float q = x * inv;
-  return x == x ? fminf(fmaxf(q, -448.f), 448.f) : x;
+  return q == q ? fminf(fmaxf(q, -448.f), 448.f) : q;
 }
+// a block whose largest is infinite has NaN for its scale: every code of it is worth NaN, the smallest root's too
+__device__ __forceinline__ float scale_of(float top) { return top < INFINITY ? top * (1.f / 448.f) : NAN; }
 template <int J> __device__ __forceinline__ int put_code(float q, unsigned up, int c) {
   return __builtin_amdgcn_cvt_sr_fp8_f32(q, (int)(up << 16 | 0x8000u), c, J);
 }
@@ -192,8 +195,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwBatch a) {
     put_codes((unsigned char*)p.m + at, (unsigned)cm, vec[u], lane, left[u]);
     put_codes((unsigned char*)p.v + at, (unsigned)cv, vec[u], lane, left[u]);
     if (lane == 0) {
-      p.m_scale[at >> 8] = top_m * (1.f / 448.f);
-      p.v_scale[at >> 8] = top_v * (1.f / 448.f);
+      p.m_scale[at >> 8] = scale_of(top_m);
+      p.v_scale[at >> 8] = scale_of(top_v);
     }
   }
 }

@@ -243,3 +243,34 @@ def test_rotary_in_place_through_a_narrower_view(B, dtype, T):
     values = x[:, 256:].clone()
     B.bk_rotary(x, freq, x[:, :256], 4, 64, pos=pos)
     assert torch.equal(x[:, :256], want) and torch.equal(x[:, 256:], values)
+
+
+# ---- AdamW ------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("bad", [float("inf"), -float("inf"), float("nan")])
+def test_adamw_8_bits_of_a_gradient_that_is_not_finite(B, bad):
+    """NaN in its element's moments, or in its block's where it sets the block's scale; nothing else differs"""
+    n, at = 1024, 300
+
+    def run(value, steps):
+        torch.manual_seed(3)
+        g, w, out = torch.randn(n, device=DEV), torch.randn(n, device=DEV), torch.empty(n, device=DEV)
+        m, v = (torch.zeros(n, dtype=torch.float8_e4m3fn, device=DEV) for _ in range(2))
+        sm, sv = torch.zeros(4, device=DEV), torch.zeros(4, device=DEV)
+        for step in range(1, steps + 1):
+            if step == 1 and value is not None:
+                g[at] = value
+            B.bk_adamw_group([g], [w], [m], [v], [out], step, m_scales=[sm], v_scales=[sv], seed=4)
+            g[at] = 1.0
+        return m.float() * sm.repeat_interleave(256), v.float() * sv.repeat_interleave(256), w, out
+    block = torch.zeros(n, dtype=torch.bool, device=DEV)
+    block[256:512] = True
+    only = torch.zeros_like(block)
+    only[at] = True
+    for steps in (1, 2):
+        clean, got = run(None, steps), run(bad, steps)
+        moments = block if abs(bad) == float("inf") else only
+        for i, (c, t) in enumerate(zip(clean, got)):
+            broken = moments if i < 2 or steps == 2 else only
+            assert bool(t[broken].isnan().all()), (i, steps)
+            assert torch.equal(t[~block], c[~block]) and bool(t[~broken].isfinite().all()), (i, steps)
