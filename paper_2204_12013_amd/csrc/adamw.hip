@@ -157,7 +157,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwBatch a) {
       m[u][j] = a.beta1 * m[u][j] + a.not_beta1 * g[u][j];
       v[u][j] = a.beta2 * v[u][j] + a.not_beta2 * g[u][j] * g[u][j];
       root[j] = sqrtf(v[u][j]);
-      w[u][j] = w[u][j] * p.keep - a.lr_c1 * m[u][j] / fmaf(root[j], a.root_c2, a.eps);
+      // all that is taken off first: 1 - lr decay in 32 bits would be off by up to 2^-25, part of a decay of 10^-6
+      w[u][j] -= fmaf(w[u][j], p.lr_decay, a.lr_c1 * m[u][j] / fmaf(root[j], a.root_c2, a.eps));
     }
     put4<STREAM>(p.master + at, w[u], vec[u], lane, left[u]);
     put_storage<STREAM>((T*)p.w + at, w[u], vec[u], lane, left[u]);
@@ -235,7 +236,7 @@ hipError_t launch_adamw(hipStream_t s, int dtype, int bits, const AdamwHyper& h,
       AdamwTensor& p = b.t[b.n++];
       p = t[i];
       b.first_wg[b.n - 1] = (int)wgs;
-      p.keep = (float)(1. - h.lr * decay[i]);
+      p.lr_decay = (float)(h.lr * decay[i]);
       p.key = mix(run + (unsigned)i * 0x85ebca6bu);
       uintptr_t at = (uintptr_t)p.g | (uintptr_t)p.master;
       at |= bits == 32 ? (uintptr_t)p.m | (uintptr_t)p.v : ((uintptr_t)p.m | (uintptr_t)p.v) << 2;

@@ -378,7 +378,7 @@ struct AdamwTensor {
   float *m_scale, *v_scale;
   void* w;
   long numel;
-  float keep;              // 1 - lr decay
+  float lr_decay;
   unsigned key;            // of the tensor's rounding
   int aligned;
 };

@@ -274,3 +274,18 @@ def test_adamw_8_bits_of_a_gradient_that_is_not_finite(B, bad):
             broken = moments if i < 2 or steps == 2 else only
             assert bool(t[broken].isnan().all()), (i, steps)
             assert torch.equal(t[~block], c[~block]) and bool(t[~broken].isfinite().all()), (i, steps)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("lr,decay", [(1e-4, 0.01), (1e-5, 0.1), (3e-5, 0.002), (1e-3, 0.1)])
+def test_adamw_decays_weights_to_their_last_bit(B, bits, lr, decay):
+    """no gradient and no moments: what is left is w - lr decay w, whose one rounding is the weight's own"""
+    n = 1 << 16
+    w0 = np.float32(np.random.default_rng(2).normal(size=n))
+    w, out, g = f32(w0), torch.empty(n, device=DEV), torch.zeros(n, device=DEV)
+    state = [torch.zeros(n, dtype=torch.float32 if bits == 32 else torch.uint8, device=DEV) for _ in range(2)]
+    scales = [[torch.zeros(n // 256, device=DEV)] for _ in range(2)] if bits == 8 else (None, None)
+    B.bk_adamw_group([g], [w], [state[0]], [state[1]], [out], 1, lr=lr, decay=decay, m_scales=scales[0], v_scales=scales[1])
+    a = w0.astype(np.float64)
+    # the decayed part has two roundings of its own (of lr decay and of the product), 2 E of it
+    within(w, a * (1 - lr * decay), E * np.abs(a) + 3 * E * lr * decay * np.abs(a), "master")
