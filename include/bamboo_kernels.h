@@ -173,7 +173,7 @@ uint64_t bk_cross_attention_scratch_floats(int batch, int sq, int sk, int heads,
  * H: entropy of the token's distribution.  mask: device bytes [T], 0 = the token does not count (its logits are not read;
  * all it gets is zeros), or NULL.  ref_logp NULL: no KL term.  Any V, strides ldl, ldd in elements; labels outside [0, V) are
  * clamped.  Outputs [T] fp32: logp, loss_tok, and, unless NULL, kl_tok (the term without its coefficient) and entropy;
- * dlogits NULL: no gradient; dlogits may be logits (with ldd = ldl).  V <= 2^27.  Logits of -inf take no part; a NaN, +inf or a row
+ * dlogits NULL: no gradient; dlogits may be logits (with ldd = ldl).  T < 2^24, V <= 2^27.  Logits of -inf take no part; a NaN, +inf or a row
  * of -inf alone makes the row NaN.  The mean over the tokens: bk_ordered_sum. */
 int bk_policy_loss(int dtype, int T, int V, const void* logits, int64_t ldl, const int32_t* labels, const uint8_t* mask,
                    const float* old_logp, const float* ref_logp, const float* adv, float clip_low, float clip_high,
@@ -185,7 +185,7 @@ int bk_policy_loss(int dtype, int T, int V, const void* logits, int64_t ldl, con
  *   margin = beta ((logp_chosen - ref_chosen) - (logp_rejected - ref_rejected))
  *   loss = -(1 - smoothing) log sigmoid(margin) - smoothing log sigmoid(-margin)
  * ref_logp[2*pairs]: the reference model's sums.  mask, labels, V, ldl: as above.  lse[T], logp[T] (0 for tokens that do not
- * count), T = 2*pairs*seq, margin[pairs], loss[pairs]: fp32 outputs; sums over a sequence are taken in 64 bits, of terms in
+ * count), T = 2*pairs*seq < 2^24, margin[pairs], loss[pairs]: fp32 outputs; sums over a sequence are taken in 64 bits, of terms in
  * 64 bits: scratch, T doubles, used by this call alone. */
 int bk_preference_loss_fwd(int dtype, int pairs, int seq, int V, const void* logits, int64_t ldl, const int32_t* labels,
                            const uint8_t* mask, const float* ref_logp, float beta, float smoothing, float* lse,
@@ -197,7 +197,7 @@ int bk_preference_loss_bwd(int dtype, int pairs, int seq, int V, const void* log
                            const uint8_t* mask, const float* lse, const float* margin, float beta, float smoothing,
                            float scale, void* dlogits, int64_t ldd, void* stream);
 
-/* One AdamW step over n tensors, step >= 1.  Host arrays of n: numel (0 is allowed), device pointers g (fp32 gradients),
+/* One AdamW step over n tensors, step >= 1.  Host arrays of n: numel (0 is allowed, below 2^34 - 1023), device pointers g (fp32 gradients),
  * master (fp32 weights), m, v, w (storage dtype, = the new master weights rounded), decay (the tensor's weight decay):
  *   m <- beta1 m + (1-beta1) g,  v <- beta2 v + (1-beta2) g^2,
  *   master <- master (1 - lr decay) - lr (m / (1-beta1^step)) / (sqrt(v / (1-beta2^step)) + eps)

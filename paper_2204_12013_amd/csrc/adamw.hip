@@ -30,6 +30,7 @@ typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 
 constexpr int kGroups = 1;                        // groups of 256 elements a wavefront takes
 constexpr int kPerWg = 4 * kGroups * 256;
+static_assert(kAdamwMost == kMaxWorkgroups * kPerWg, "a tensor is one launch's at most");
 
 template <bool STREAM> __device__ __forceinline__ f32x4 load4(const float* p) {
   return STREAM ? __builtin_nontemporal_load((const f32x4*)p) : *(const f32x4*)p;
@@ -232,7 +233,7 @@ hipError_t launch_adamw(hipStream_t s, int dtype, int bits, const AdamwHyper& h,
     for (; i < n && b.n < kAdamwTensors; ++i) {
       if (t[i].numel == 0) continue;
       const long need = (t[i].numel + kPerWg - 1) / kPerWg;
-      if (b.n > 0 && wgs + need > 0x7fffffffL) break;
+      if (b.n > 0 && wgs + need > kMaxWorkgroups) break;
       AdamwTensor& p = b.t[b.n++];
       p = t[i];
       b.first_wg[b.n - 1] = (int)wgs;

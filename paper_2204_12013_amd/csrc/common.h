@@ -293,6 +293,9 @@ hipError_t launch_ordered_sum(hipStream_t s, long n, const float* in, float scal
 inline bool streams_past_cache(long bytes) { return bytes > (384L << 20); }
 
 // ---- operators around the stage ------------------------------------------------------
+// A launch has fewer than 2^32 threads in each dimension: workgroups of 256 that it can have.
+constexpr long kMaxWorkgroups = (1L << 24) - 1;
+
 // rotary positions: see bk_rotary; tokens, heads_per_wg: what one workgroup takes (set by the launcher)
 struct RotaryDesc {
   const void* x;
@@ -371,6 +374,7 @@ hipError_t launch_cross_dkv_f32(hipStream_t s, int dtype, const CrossDesc& d);
 
 // AdamW on many tensors: see bk_adamw_group
 constexpr int kAdamwTensors = 40;      // of one launch: their descriptors are kernel arguments, 4 KB at most
+constexpr long kAdamwMost = kMaxWorkgroups * 1024;      // elements of one tensor
 struct AdamwTensor {
   const float* g;
   float* master;

@@ -120,7 +120,8 @@ long up4(long n) { return (n + 3) / 4 * 4; }
 // fp32, 13 x 502 x 514, 32 heads over 4 of 128 (260, four more than CUs), 2231 us as one, 1351 + 57 as nine.
 int parts(long owned, long streamed, long pairs, long floats, float tile_us, bool mfma, int least) {
   const long wgs = (owned + 127) / 128 * pairs, tiles = (streamed + 63) / 64;
-  const int most = (int)(tiles / least < 64 ? tiles / least : 64);
+  const long room = kMaxWorkgroups / wgs < 64 ? kMaxWorkgroups / wgs : 64;
+  const int most = (int)(tiles / least < room ? tiles / least : room);
   int best = 1;
   float best_us = 0.f;
   for (int n = 1; n <= most || n == 1; ++n) {

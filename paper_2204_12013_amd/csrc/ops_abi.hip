@@ -370,7 +370,7 @@ int bk_policy_loss(int dtype, int T, int V, const void* logits, int64_t ldl, con
                    const float* old_logp, const float* ref_logp, const float* adv, float clip_low, float clip_high,
                    float kl_coef, float ent_coef, float scale, float* logp, float* loss_tok, float* kl_tok,
                    float* entropy, void* dlogits, int64_t ldd, void* stream) {
-  if ((dtype != 0 && dtype != 1) || T <= 0 || V <= 0 || V > kMaxVocab || ldl < V) return BAMBOO_E_ARG;
+  if ((dtype != 0 && dtype != 1) || T <= 0 || T > kMaxWorkgroups || V <= 0 || V > kMaxVocab || ldl < V) return BAMBOO_E_ARG;
   if (!logits || !labels || !old_logp || !adv || !logp || !loss_tok || !element_aligned(dtype, logits)) return BAMBOO_E_ARG;
   if (!(clip_low >= 0.f && clip_low <= 1.f && clip_high >= 0.f)) return BAMBOO_E_ARG;
   if (dlogits && bad_gradient(dtype, T, V, logits, ldl, dlogits, ldd)) return BAMBOO_E_ARG;
@@ -386,7 +386,7 @@ int bk_policy_loss(int dtype, int T, int V, const void* logits, int64_t ldl, con
 static int preference_desc(PreferenceDesc& a, int dtype, int pairs, int seq, int V, const void* logits, int64_t ldl,
                            const int32_t* labels, const uint8_t* mask, float beta, float smoothing) {
   if ((dtype != 0 && dtype != 1) || pairs <= 0 || seq <= 0 || V <= 0 || V > kMaxVocab || ldl < V) return BAMBOO_E_ARG;
-  if ((int64_t)2 * pairs * seq > 0x7fffffff || !logits || !labels || !element_aligned(dtype, logits)) return BAMBOO_E_ARG;
+  if ((int64_t)2 * pairs * seq > kMaxWorkgroups || !logits || !labels || !element_aligned(dtype, logits)) return BAMBOO_E_ARG;
   if (!(smoothing >= 0.f && smoothing <= 1.f)) return BAMBOO_E_ARG;
   memset(&a, 0, sizeof(a));
   a.logits = logits; a.ldl = ldl; a.pairs = pairs; a.seq = seq; a.V = V; a.labels = labels; a.mask = mask; a.beta = beta;
@@ -434,7 +434,7 @@ int bk_adamw_group(int dtype, int moment_bits, int n, const int64_t* numel, cons
       AdamwTensor& p = t[i];
       memset(&p, 0, sizeof(p));
       p.numel = numel[i];
-      if (p.numel < 0 || p.numel > (int64_t)1 << 40) return BAMBOO_E_ARG;
+      if (p.numel < 0 || p.numel > kAdamwMost) return BAMBOO_E_ARG;
       if (p.numel == 0) continue;
       p.g = g[i]; p.master = master[i]; p.m = m[i]; p.v = v[i]; p.w = w[i];
       if (!p.g || !p.master || !p.m || !p.v || !p.w || !element_aligned(dtype, p.w)) return BAMBOO_E_ARG;

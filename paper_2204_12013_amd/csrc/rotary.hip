@@ -115,6 +115,7 @@ hipError_t rotary_launch(hipStream_t s, RotaryDesc a) {
   a.tokens = (int)(row >= 1024 ? 1 : (1024 + row - 1) / row);
   if (a.tokens > kRotTokens) a.tokens = kRotTokens;
   while (a.tokens > 1 && (a.T + a.tokens - 1) / a.tokens < 512) a.tokens /= 2;
+  while (a.tokens < kRotTokens && (a.T + (long)a.tokens - 1) / a.tokens > kMaxWorkgroups) ++a.tokens;
   const int blocks = (a.T + a.tokens - 1) / a.tokens;
   int parts = 1;
   while (blocks * parts < 512 && row / (parts * 2) >= kRotThreads) parts *= 2;

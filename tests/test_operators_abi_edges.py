@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2204_12013_amd import binding as B
-from test_operators_abi import CROSS_BWD, P, P2, POLICY, ROTARY
+from test_operators_abi import CROSS_BWD, P, P2, POLICY, PREF, PREF_BWD, ROTARY, _adamw
 
 
 def test_the_row_distance_of_a_single_row_says_nothing():
@@ -18,3 +18,22 @@ def test_the_row_distance_of_a_single_row_says_nothing():
     for change in (dict(ldx=300), dict(ldy=300), dict(ldx=128, ldy=1 << 33), dict(y=P + 2 * 128, ldy=300)):
         assert B.lib.bk_rotary(*dict(row, **change).values()) == B.E_HIP
     assert B.lib.bk_policy_loss(*dict(POLICY, T=1, ldd=200).values()) == B.E_HIP
+
+
+MOST = (1 << 24) - 1          # workgroups of 256 threads in a launch
+
+
+@pytest.mark.parametrize("name,good,bad,last", [
+    ("bk_policy_loss", POLICY, dict(T=MOST + 1), dict(T=MOST)),
+    ("bk_preference_loss_fwd", PREF, dict(pairs=MOST // 2 + 1, seq=1), dict(pairs=MOST // 2, seq=1)),
+    ("bk_preference_loss_bwd", PREF_BWD, dict(pairs=1, seq=MOST // 2 + 1), dict(pairs=1, seq=MOST // 2))])
+def test_more_rows_than_a_launch_has_workgroups_are_refused(name, good, bad, last):
+    assert getattr(B.lib, name)(*dict(good, **bad).values()) == B.E_ARG
+    if not torch.cuda.is_available():      # the addresses are none: without a GPU the launch itself is what fails
+        assert getattr(B.lib, name)(*dict(good, **last).values()) == B.E_HIP
+
+
+def test_more_elements_than_a_launch_can_take_are_refused():
+    assert _adamw(numel=(8, MOST * 1024 + 1), master=(P, P + 4096)) == B.E_ARG
+    if not torch.cuda.is_available():
+        assert _adamw(numel=(8, MOST * 1024), master=(P, P + 4096)) == B.E_HIP
