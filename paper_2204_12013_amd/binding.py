@@ -642,11 +642,16 @@ def _mask(t, n, dev, where):
     return _vec(t, n, torch.bool if t is not None and t.dtype == torch.bool else torch.uint8, dev, where)
 
 
+_MOST = 0x7FFFFFFF                                          # sizes are handed over in 32 bits
+
+
 def _first(t, where):
     """(rows, columns, dtype, its code, device) of the matrix that the others go by."""
     if t.dim() != 2 or t.dtype not in _ACT:
         _refuse(where)
     (rows, cols), dtype = t.shape, t.dtype
+    if rows > _MOST or cols > _MOST:
+        _refuse(where)
     return rows, cols, dtype, _ACT[dtype], _get_device(t)
 
 
@@ -704,7 +709,8 @@ def bk_rotary(x, freq, y, heads, d, pos=None, seq=1, interleaved=False, inverse=
 def _cross(q, k, v, batch, heads, kv_heads, kv_len, where):
     """Sizes, then the arguments that both directions share: (dtype, device, rows and columns of q, of k), sizes, addresses"""
     rows, cols, dtype, code, dev = _first(q, where)
-    if batch <= 0 or heads <= 0 or kv_heads <= 0 or rows % batch or cols % heads or k.dim() != 2 or k.shape[0] % batch:
+    if batch <= 0 or heads <= 0 or kv_heads <= 0 or rows % batch or cols % heads or k.dim() != 2 or k.shape[0] % batch or \
+            k.shape[0] > _MOST:
         _refuse(where)
     d, keys = cols // heads, k.shape[0]
     pq, ldq = _rows(q, where, rows, cols, dtype, dev)

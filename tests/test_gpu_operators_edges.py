@@ -289,3 +289,16 @@ def test_adamw_decays_weights_to_their_last_bit(B, bits, lr, decay):
     a = w0.astype(np.float64)
     # the decayed part has two roundings of its own (of lr decay and of the product), 2 E of it
     within(w, a * (1 - lr * decay), E * np.abs(a) + 3 * E * lr * decay * np.abs(a), "master")
+
+
+# ---- sizes -------------------------------------------------------------------------------------------
+
+def test_sizes_that_pass_32_bits_are_refused(B):
+    """handed over in 32 bits they would be those of four rows"""
+    x = torch.empty(2 ** 32 + 4, 2, dtype=torch.bfloat16, device=DEV)
+    freq, _ = B.bk_rotary_frequencies(2)
+    q, lse = torch.ones(1, 2, dtype=torch.bfloat16, device=DEV), torch.empty(1, device=DEV)
+    for call in (lambda: B.bk_rotary(x, freq, x, 1, 2), lambda: B.bk_cross_attention_fwd(q, x, x, q.clone(), lse, 1, 1)):
+        with pytest.raises(B.BambooError) as e:
+            call()
+        assert e.value.status == B.E_ARG
