@@ -164,6 +164,8 @@ int bk_cross_attention_bwd(int dtype, int impl, int batch, int sq, int sk, int h
                            int64_t ldq, const void* k, const void* v, int64_t ldkv, const int32_t* kv_len,
                            const void* ctx, int64_t ldc, const float* lse, const void* dctx, int64_t lddc, void* dq,
                            int64_t lddq, void* dk, void* dv, int64_t lddkv, float* scratch, void* stream);
+/* 0 for sizes that the calls refuse (the product of batch, kv_heads and the larger of sk and sq * heads / kv_heads has to stay below
+ * 2^31). */
 uint64_t bk_cross_attention_scratch_floats(int batch, int sq, int sk, int heads, int kv_heads, int d);
 
 /* Clipped policy loss with a KL and an entropy term, and its gradient in the same pass.  Per token t, with

@@ -289,22 +289,22 @@ int bk_rotary_frequencies(int rot, double base, int scaling, double factor, int 
   return BAMBOO_OK;
 }
 
+static bool cross_sizes(int batch, int sq, int sk, int heads, int kv_heads, int d) {
+  if (batch <= 0 || sq <= 0 || sk <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || d <= 0 || d > 128) return false;
+  // row numbers and workgroups are 32-bit
+  const int64_t group = heads / kv_heads, rows = sq * group, pairs = (int64_t)batch * kv_heads;
+  const int64_t most = rows > sk ? rows : sk;
+  return rows <= 0x7fffff00 && rows * group <= 0xffffffffLL && sk <= 0x7fffff00 && pairs <= 0x7fffffff &&
+         (most + 1024) * pairs <= 0x7fffffff && pairs * most * 2 * d / 256 + 1 <= 0x7fffffff;
+}
 static int cross_desc(CrossDesc& a, int dtype, int impl, int batch, int sq, int sk, int heads, int kv_heads, int d, const void* q,
                       int64_t ldq, const void* k, const void* v, int64_t ldkv, const int32_t* kv_len, const void* ctx, int64_t ldc,
                       const float* lse, float* scratch) {
-  if ((dtype != 0 && dtype != 1) || impl < 0 || impl > 2 || batch <= 0 || sq <= 0 || sk <= 0 || heads <= 0 || kv_heads <= 0 ||
-      heads % kv_heads || d <= 0 || d > 128)
-    return BAMBOO_E_ARG;
+  if ((dtype != 0 && dtype != 1) || impl < 0 || impl > 2 || !cross_sizes(batch, sq, sk, heads, kv_heads, d)) return BAMBOO_E_ARG;
   if (!q || !k || !v || !ctx || !lse) return BAMBOO_E_ARG;
   for (const void* p : {q, k, v, ctx})
     if (!element_aligned(dtype, p)) return BAMBOO_E_ARG;
   if (ldq < (int64_t)heads * d || ldkv < (int64_t)kv_heads * d || ldc < (int64_t)heads * d) return BAMBOO_E_ARG;
-  // row numbers and workgroups are 32-bit
-  const int64_t group = heads / kv_heads, rows = sq * group, pairs = (int64_t)batch * kv_heads;
-  const int64_t most = rows > sk ? rows : sk;
-  if (rows > 0x7fffff00 || rows * group > 0xffffffffLL || sk > 0x7fffff00 || pairs > 0x7fffffff ||
-      (most + 1024) * pairs > 0x7fffffff || pairs * most * 2 * d / 256 + 1 > 0x7fffffff)
-    return BAMBOO_E_ARG;
   if ((!scratch && bk_cross_attention_scratch_floats(batch, sq, sk, heads, kv_heads, d) > 0) || ((uintptr_t)scratch & 15)) return BAMBOO_E_ARG;
   memset(&a, 0, sizeof(a));
   a.B = batch; a.sq = sq; a.sk = sk; a.heads = heads; a.kv_heads = kv_heads; a.d = d;
@@ -320,7 +320,7 @@ static Matrix key_rows(const CrossDesc& a, int dtype, const void* p, int64_t ld)
 }
 
 uint64_t bk_cross_attention_scratch_floats(int batch, int sq, int sk, int heads, int kv_heads, int d) {
-  if (batch <= 0 || sq <= 0 || sk <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || d <= 0 || d > 128) return 0;
+  if (!cross_sizes(batch, sq, sk, heads, kv_heads, d)) return 0;
   return cross_attention_scratch_floats(batch, sq, sk, heads, kv_heads, d);
 }
 

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_2204_12013_amd import binding as B
-from test_operators_abi import CROSS_BWD, P, P2, POLICY, PREF, PREF_BWD, ROTARY, _adamw
+from test_operators_abi import CROSS, CROSS_BWD, P, P2, POLICY, PREF, PREF_BWD, ROTARY, _adamw
 
 
 def test_the_row_distance_of_a_single_row_says_nothing():
@@ -37,3 +37,13 @@ def test_more_elements_than_a_launch_can_take_are_refused():
     assert _adamw(numel=(8, MOST * 1024 + 1), master=(P, P + 4096)) == B.E_ARG
     if not torch.cuda.is_available():
         assert _adamw(numel=(8, MOST * 1024), master=(P, P + 4096)) == B.E_HIP
+
+
+@pytest.mark.parametrize("sizes", [(1, 1 << 30, 4, 1 << 30, 1, 128), (1 << 20, 1 << 20, 1 << 20, 8, 8, 64), (1 << 30, 1, 1, 4, 4, 64),
+                                   (1, 1 << 16, 1, 1 << 16, 1, 1), (1, 1, 0x7FFFFFFF, 1, 1, 1)])
+def test_no_scratch_for_sizes_that_are_refused(sizes):
+    """their products pass 64 bits, or what a launch can have"""
+    batch, sq, sk, heads, kv_heads, d = sizes
+    assert B.lib.bk_cross_attention_scratch_floats(*sizes) == 0
+    big = dict(batch=batch, sq=sq, sk=sk, heads=heads, kv_heads=kv_heads, d=d, ldq=heads * d, ldkv=kv_heads * d, ldc=heads * d)
+    assert B.lib.bk_cross_attention_fwd(*dict(CROSS, **big).values()) == B.E_ARG
