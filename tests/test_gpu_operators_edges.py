@@ -302,3 +302,57 @@ def test_sizes_that_pass_32_bits_are_refused(B):
         with pytest.raises(B.BambooError) as e:
             call()
         assert e.value.status == B.E_ARG
+
+
+# ---- graphs ------------------------------------------------------------------------------------------
+
+def test_losses_keys_and_8_bit_moments_captured_and_replayed(B):
+    """what replays with new inputs in its buffers, key lengths among them, with eager calls of the same kind in between"""
+    pairs, seq, V, batch, sk, heads, d, n = 2, 3, 4099, 2, 900, 4, 64, 3000
+    T = 2 * pairs * seq
+    bf = lambda *s: torch.randn(*s, device=DEV).bfloat16()
+    z, z2, q, kv, g = bf(T, V), bf(T, V), bf(batch, heads * d), bf(batch * sk, 2 * heads * d), bf(batch, heads * d)
+    lens, grad, ref = torch.tensor([sk, 0], dtype=torch.int32, device=DEV), torch.randn(n, device=DEV), torch.randn(2 * pairs, device=DEV)
+    lab, mask = torch.randint(0, V, (T,), dtype=torch.int32, device=DEV), torch.ones(T, dtype=torch.uint8, device=DEV)
+    one = torch.ones(T, device=DEV)
+    master, codes, scales = torch.randn(n, device=DEV), torch.randint(0, 120, (2, n), dtype=torch.uint8, device=DEV), torch.rand(2, 12, device=DEV)
+    f = lambda *s: torch.empty(*s, device=DEV)
+
+    def bufs():
+        return dict(lse=f(T), logp=f(T), seqs=f(2 * pairs), margin=f(pairs), loss=f(pairs), d=torch.empty_like(z), d2=torch.empty_like(z),
+                    tok=f(T), kl=f(T), ent=f(T), logp2=f(T), ctx=torch.empty_like(q), st=f(batch, heads, 1), dq=torch.empty_like(q),
+                    dkv=torch.empty_like(kv), w=f(n), out=f(n), c=torch.empty_like(codes), s=torch.empty_like(scales))
+
+    def once(b):
+        H = heads * d
+        B.bk_preference_loss_fwd(z, lab, ref, b["lse"], b["logp"], b["seqs"], b["margin"], b["loss"], 0.1, 0.1, mask=mask)
+        B.bk_preference_loss_bwd(z, lab, b["lse"], b["margin"], b["d"], 0.1, 0.1, mask=mask)
+        B.bk_policy_loss(z2, lab, -one, one, b["logp2"], b["tok"], b["d2"], mask=mask, ref_logp=-one, kl_tok=b["kl"], entropy=b["ent"],
+                         kl_coef=0.1, ent_coef=0.1)
+        B.bk_cross_attention_fwd(q, kv[:, :H], kv[:, H:], b["ctx"], b["st"], batch, heads, kv_len=lens)
+        B.bk_cross_attention_bwd(q, kv[:, :H], kv[:, H:], b["ctx"], b["st"], g, b["dq"], b["dkv"][:, :H], b["dkv"][:, H:], batch, heads,
+                                 kv_len=lens)
+        for k, t in (("w", master), ("c", codes), ("s", scales)):
+            b[k].copy_(t)
+        B.bk_adamw_group([grad], [b["w"]], [b["c"][0]], [b["c"][1]], [b["out"]], 7, m_scales=[b["s"][0]], v_scales=[b["s"][1]], seed=3)
+        return b
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        once(bufs())
+    torch.cuda.current_stream().wait_stream(side)
+    held, graph = bufs(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        once(held)
+    for k in range(3):
+        for t in (z, z2, q, kv, g, grad, ref, master):
+            t.copy_(torch.randn(t.shape, device=DEV))
+        lab.random_(0, V)
+        mask.random_(0, 2)
+        lens.copy_(torch.tensor([[1, sk], [0, 0], [65, 700]][k], dtype=torch.int32))
+        want = once(bufs())
+        graph.replay()
+        torch.cuda.synchronize()
+        for name in held:
+            a, b = held[name], want[name]
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8)), (k, name)
