@@ -153,8 +153,10 @@ int bk_rotary_frequencies(int rot, double base, int scaling, double factor, int 
  * and values behind them are never read.  ctx[batch*sq, heads*d] (row stride ldc), lse[batch,heads,sq] fp32.  A sample
  * without keys has ctx = 0 and lse = -inf.
  * scratch: fp32, bk_cross_attention_scratch_floats(..) floats, 16-byte aligned, used by this call alone.
- * impl: 0 automatic, 1 fp32 arithmetic on the matrix cores, 2 bf16 on them (BAMBOO_E_STATE for fp32 tensors).  bf16 is fastest
- * with d 64 or 128, strides multiples of 8 and pointers aligned to 16 bytes. */
+ * impl: 0 automatic (2 for bf16 tensors, 1 for fp32 ones), 1 fp32 arithmetic on the matrix cores, 2 bf16 on them (BAMBOO_E_STATE for
+ * fp32 tensors).  2 rounds the probabilities, and in the backward dS, to bf16 for the products that follow: gradients are 0.0022 to
+ * 0.0029 of their norm off and ctx up to 0.0025, where the one rounding of a result is 0.0017; 1 on bf16 tensors rounds results alone, at
+ * a sixteenth of the matrix rate.  Scores are taken to stay within 10^29.  bf16 is fastest with d 64 or 128, strides multiples of 8 and pointers aligned to 16 bytes. */
 int bk_cross_attention_fwd(int dtype, int impl, int batch, int sq, int sk, int heads, int kv_heads, int d, const void* q,
                            int64_t ldq, const void* k, const void* v, int64_t ldkv, const int32_t* kv_len, void* ctx,
                            int64_t ldc, float* lse, float* scratch, void* stream);
@@ -207,7 +209,7 @@ int bk_preference_loss_bwd(int dtype, int pairs, int seq, int V, const void* log
  * [ceil(numel/256)]: element i of m is code * m_scale[i/256], the ROOT of element i of v is code * v_scale[i/256]; all
  * zero bits are zero moments.  The step uses the moments before they are rounded to codes; the rounding goes up or down by
  * bits that depend on (seed, step, the tensor's place in the list, the element) alone, so that replicas that make the
- * same calls stay equal to the bit.  With 8 bits a gradient that is NaN makes its element's moments NaN, an infinite one its
+ * same calls stay equal to the bit (a captured call repeats its own step number and rate).  With 8 bits a gradient that is NaN makes its element's moments NaN, an infinite one its
  * whole block's (and a finite one whose square is not, the block's second moments).  No two tensors may overlap.  Any alignment of an element; the fast form takes pointers aligned to 16
  * bytes (w and codes: to four elements). */
 int bk_adamw_group(int dtype, int moment_bits, int n, const int64_t* numel, const float* const* g, float* const* master,

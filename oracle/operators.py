@@ -137,6 +137,7 @@ def e4m3(codes):
 
 
 def _mix(x):
+    """an integer hash of 32 bits (C. Wellons, "Prospecting for Hash Functions", 2018)"""
     m = np.uint64(0xFFFFFFFF)
     x = np.asarray(x, np.uint64)
     x = x ^ (x >> np.uint64(16))

@@ -6,8 +6,8 @@
 // HBM-bound: per parameter 28 bytes of gradient, master weight and moments and the storage copy, or 16 + 1/16 with
 // moments in 8 bits.  One launch takes up to kAdamwTensors tensors, whose descriptors travel in the kernel's arguments
 // (nothing on the device has to outlive the call, and a captured graph holds its own copy); a workgroup finds its tensor
-// with one load per lane and a ballot.  75.6 M parameters in 72 tensors: 386 us, 5.9 TB/s (two groups of 256 a wavefront 427 us,
-// storage weights kept in the caches 402 us); 184 M with moments in 8 bits: 595 us, 5.6 TB/s (codes made by comparisons and shifts
+// with one load per lane and a ballot.  75.6 M parameters in 72 tensors: 382 us, 5.9 TB/s (two groups of 256 a wavefront 427 us,
+// storage weights kept in the caches 402 us); 184 M with moments in 8 bits: 556 to 632 us, 5.3 to 6.0 TB/s (codes made by comparisons and shifts
 // 658 us: the arithmetic was as long as the traffic).
 //
 // 8 bits: blocks of 256 elements share a scale (largest / 448) and each element is an e4m3 code, value = code * scale.
@@ -97,6 +97,8 @@ __device__ __forceinline__ f32x4 decode(unsigned c, float scale) {
   v[3] = __builtin_amdgcn_cvt_f32_fp8((int)c, 3) * scale;
   return v;
 }
+// An integer hash of 32 bits: shifts and multipliers are a published set, found by a search for the least bias between input and
+// output bits (C. Wellons, "Prospecting for Hash Functions", 2018).
 __host__ __device__ __forceinline__ unsigned mix(unsigned x) {
   x ^= x >> 16;
   x *= 0x7feb352du;

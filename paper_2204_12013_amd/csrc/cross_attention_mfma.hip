@@ -8,9 +8,9 @@
 //
 // Probabilities and dS are rounded to bf16 as operands of the second products: dQ of 8 x 512 x 333 is 0.0025 of its norm off, 0.0017
 // of that the rounding of the result itself.
-// Large problems are bound by the matrix instructions (1 x 2048 x 4096, 96 heads over 8 of 128: forward 400 us, 1030 TFLOP/s; dQ
-// 530 us, 1160; dK and dV 820 us, 1000; a large library product 1210), those of few tiles by a wavefront's own chain of vector
-// and matrix instructions at two to three wavefronts a SIMD (8 x 512 x 333, 16 heads of 64: 12.4, 16.4 and 21.5 us; 1.25 us a
+// Large problems are bound by the matrix instructions (1 x 2048 x 4096, 96 heads over 8 of 128: forward 419 us, 980 TFLOP/s; dQ
+// 523 us, 1180; dK and dV 843 us, 980; a large library product 1210), those of few tiles by a wavefront's own chain of vector
+// and matrix instructions at two to three wavefronts a SIMD (8 x 512 x 333, 16 heads of 64: 13.2, 17.0 and 21.9 us; 1.25 us a
 // tile of 64 keys in the forward) and by what a launch takes to start and end.
 #include "attention_tiles.h"
 #include "cross_rows.h"

@@ -9,9 +9,9 @@
 // on chip.  It is held in registers, in the storage type: a workgroup of 256 to 1024 threads requests its whole row at
 // once (up to 16 vectors of 16 bytes a thread), which also is what keeps enough loads in flight.  Rows beyond that are
 // read again.  All sums are in 32 bits, in a fixed order; those over a sequence in 64.
-// 4096 x 50304 bf16 with KL and entropy, a quarter of the tokens left out (721 MB): 136 us, 5.3 TB/s (191 us with three
+// 4096 x 50304 bf16 with KL and entropy, a quarter of the tokens left out (721 MB): 139 us, 5.2 TB/s (191 us with three
 // operations to an exponent, comparisons with the label, and 1024 threads a row, of which a CU holds one workgroup).  Preference
-// loss 4096 x 30528 bf16, half of the tokens left out: log-probabilities 23 us, gradient 50 us.
+// loss 4096 x 30528 bf16, half of the tokens left out: log-probabilities 25 us, gradient 51 us.
 #include <math.h>
 
 #include <type_traits>
@@ -471,13 +471,22 @@ __global__ __launch_bounds__(256) void preference_bwd_kernel(PreferenceDesc a) {
 }
 
 // Calls go(threads, chunks) with the smallest workgroup and number of chunks a thread that hold V elements of T; where the
-// rows do not fill the chip, with more threads: a row's time is then its own chain of arithmetic and trips to memory.
+// rows do not fill the chip, with more threads: a row's time is then its own chain of arithmetic and trips to memory.  With 1024
+// threads always and never, us (8 to 256 rows: a workgroup a CU at most):
+//                    8 rows       48         128        256        320        512        1024       2048
+//   bf16  17000    8.8 /  9.4   8.9 /  9.6   9.4 / 10.0  11.2 / 11.5  14.3 / 13.7  15.8 / 15.7  23.4 / 21.8   39 /  38
+//   bf16  30528    9.9 / 11.3  10.3 / 11.9  11.9 / 13.3  14.5 / 15.5  19.0 / 20.2  19.8 / 21.2  33.7 / 33.9   57 /  58
+//   bf16  50304   12.3 / 12.6  12.9 / 13.3  15.4 / 15.9  19.5 / 19.7  25.3 / 24.6  35.1 / 31.9  59.1 / 51.8  101 /  86
+//   fp32   8300    7.7 /  9.1   7.9 /  9.3   8.6 /  9.7  10.1 / 11.1  12.1 / 12.3  13.5 / 13.9  21.0 / 17.8   36 /  36
+//   fp32  16000    8.6 / 11.6   9.3 / 12.2  10.5 / 13.1  13.0 / 15.3  15.2 / 16.7  17.0 / 20.5  33.2 / 29.9   57 /  64
+//   fp32  32003   11.0 / 12.5  12.2 / 13.8  14.8 / 16.3  18.6 / 19.5  30.3 / 28.2  36.4 / 31.8  67.8 / 61.5  112 / 112
+// Up to 256 rows more threads never lose; beyond, which of the two wins changes with the length, and the most they win is 17 %.
 template <typename T, typename GO>
 hipError_t by_row_length(int rows, int V, GO go) {
   const int chunks = (V + Chunk<T>::N - 1) / Chunk<T>::N;
 #define BAMBOO_ROW(NT, NC) \
   if (chunks <= NT * NC) return go(std::integral_constant<int, NT>(), std::integral_constant<int, NC>())
-  if (rows <= 256 && chunks > 2048) {      // 48 rows of 32003 in fp32: 10.2 us with 512 threads, 8.8 with 1024
+  if (rows <= 256 && chunks > 2048) {
     BAMBOO_ROW(1024, 4);
     BAMBOO_ROW(1024, 8);
   }
@@ -510,7 +519,16 @@ hipError_t policy_launch(hipStream_t s, const PolicyDesc& a) {
   });
 }
 // Read once, so nothing is held.  Few rows: their time is a chain of trips to memory, fewer with more threads (held in
-// registers, for the cheaper exponents, 96 rows of 50257 took 7.6 us in the place of 7.2).
+// registers, for the cheaper exponents, 96 rows of 50257 took 7.6 us in the place of 7.2).  With 256 and with 1024 threads, us, the
+// launch that sums the sequences included:
+//                  48 rows      128        256        384        512        768        1024       2048
+//   bf16   1000   5.8 /  5.9   5.9 /  6.1   5.8 /  6.1   6.2 /  6.7   6.1 /  6.7   6.4 /  7.8   6.9 /  8.6   7.5 / 12.1
+//   bf16   8000   6.4 /  6.4   6.5 /  6.5   6.7 /  6.8   7.4 /  7.9   7.8 /  8.1   9.2 /  9.5   9.9 / 10.9  12.4 / 16.2
+//   bf16  30528   8.6 /  7.7   9.4 /  8.2  10.4 /  9.8  11.5 / 12.2  12.5 / 12.4  14.9 / 15.1  16.4 / 17.5  31.2 / 31.5
+//   bf16  50257  11.8 /  9.6  13.7 / 10.6  14.2 / 11.3  15.8 / 14.8  17.0 / 15.7  25.1 / 25.1  32.9 / 31.2  54.3 / 53.1
+//   fp32  32003  11.7 /  8.7  12.4 /  9.3  13.5 / 11.0  14.7 / 14.2  16.4 / 16.6  24.9 / 24.3  31.9 / 30.8  54.1 / 52.1
+// 1024 threads win up to 24 % for long rows below 512 of them and lose up to 10 % for short ones, whose whole call is 6 us; from 512
+// rows on they win 8 % at most and lose up to 38 %.
 template <typename T>
 hipError_t token_logp_launch(hipStream_t s, const PreferenceDesc& a, unsigned rows) {
   if (rows >= 512) hipLaunchKernelGGL((token_logp_kernel<T, 256>), dim3(rows), dim3(256), 0, s, a);
