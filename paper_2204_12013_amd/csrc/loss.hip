@@ -341,9 +341,11 @@ __global__ __launch_bounds__(NT) void policy_loss_kernel(PolicyDesc a) {
   float loss = -(counts ? free : held), coef = counts ? -free : 0.f, kl = 0.f;
   if (a.ref_logp != nullptr) {
     const float away = (ref - below) + r.log_s, grown = expm1f(away);
-    kl = grown - away;
-    loss = fmaf(a.kl_coef, kl, loss);
-    coef = fmaf(-a.kl_coef, grown, coef);
+    kl = grown < INFINITY ? grown - away : grown;               // exp(u) - u - 1 grows without bound with u
+    if (a.kl_coef != 0.f) {                                     // an infinite term without weight adds nothing
+      loss = fmaf(a.kl_coef, kl, loss);
+      coef = fmaf(-a.kl_coef, grown, coef);
+    }
   }
   if (ENT) loss = fmaf(-a.ent_coef, r.entropy, loss);
   if (threadIdx.x == 0) {

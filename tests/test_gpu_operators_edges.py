@@ -193,6 +193,25 @@ def test_preference_gradient_of_pairs_that_are_told_apart_well(B, dtype, smoothi
     within(d, c * (hit - p), bound + (unit(dtype) + 2 * E) * np.abs(c * (hit - p)) + 1e-38, "dlogits")
 
 
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("V", [100, 2051, 140001])
+def test_policy_loss_of_a_label_that_cannot_be(B, dtype, V):
+    """its probability is 0 and its KL term infinite, not NaN; without weight the term adds nothing to loss and gradient"""
+    T, label = 4, 7
+    act = torch.bfloat16 if dtype == 1 else torch.float32
+    z = torch.randn(T, V, device=DEV).to(act)
+    z[1, label] = z[2, 3] = -float("inf")
+    lab, one = torch.full((T,), label, dtype=torch.int32, device=DEV), torch.ones(T, device=DEV)
+    for coef in (0.0, 0.1):
+        logp, loss, kl, ent = (torch.empty(T, device=DEV) for _ in range(4))
+        d = torch.empty_like(z)
+        B.bk_policy_loss(z, lab, -one, one, logp, loss, d, ref_logp=-one, kl_tok=kl, entropy=ent, kl_coef=coef, ent_coef=0.1)
+        assert float(logp[1]) == -np.inf and float(kl[1]) == np.inf
+        fine = torch.tensor([True, coef == 0.0, True, True], device=DEV)
+        assert bool(loss[fine].isfinite().all()) and bool(d[fine].isfinite().all()) and bool(ent.isfinite().all())
+        assert coef == 0.0 or float(loss[1]) == np.inf
+
+
 # ---- attention over an encoder's states -------------------------------------------------------------
 
 @pytest.mark.parametrize("garbage", [float("nan"), float("inf")])
