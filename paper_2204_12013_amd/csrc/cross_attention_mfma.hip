@@ -311,7 +311,7 @@ __global__ __launch_bounds__(256, PAD && D == 128 ? 1 : 2) void cross_dq_mfma_ke
     *p = kb + at_row;
     *q = vb + at_row;
   };
-  // tile t of this part to `slot`, at once
+  // tile t of this part (-t0: the sample's first) to `slot`, at once
   const auto bring = [&](int t, int slot) {
     if constexpr (PAD) {
       pad.fetch(keys, t0 + t, d);
@@ -321,18 +321,21 @@ __global__ __launch_bounds__(256, PAD && D == 128 ? 1 : 2) void cross_dq_mfma_ke
       copy.issue(vb, t0 + t, ring + slot * 2 * TB + TB);
     }
   };
-  if (nt > 0) bring(0, 0);
+  const int all = (len + TILE - 1) / TILE;
+  const bool few = nt > 0 && all <= 2;
+  if (nt > 0) bring(few ? -t0 : 0, 0);
   const f32x16 zero16 = {};
-  if (a.splits == 1 && nt > 0 && nt <= 2) {
-    // Few keys: both tiles fit the ring, and delta is the sum of p dP as the scores give it.  ctx has been rounded to bf16, and
-    // what that is off by does not average out over few keys (error of dQ: 3 keys 0.0043 of its norm, 0.0024 this way; at
-    // 333 keys the roundings of dS and dQ themselves are 0.0024 and those of delta 0.0007).
-    if (nt == 2) bring(1, 1);
+  if (few) {
+    // Few keys: both tiles of the sample fit the ring, and delta is the sum of p dP as the scores give it.  ctx has been rounded to
+    // bf16, and what that is off by does not average out over few keys (error of dQ: 3 keys 0.0043 of its norm, 0.0024 this way; at
+    // 333 keys the roundings of dS and dQ themselves are 0.0024 and those of delta 0.0007).  Where the two are of different parts,
+    // each part forms delta from both.
+    if (all == 2) bring(1 - t0, 1);
     wait_tiles<0>();
     __syncthreads();
     delta = 0.f;
     if (busy)
-      for (int t = 0; t < nt; ++t) {
+      for (int t = 0; t < all; ++t) {
         const unsigned buf = ring + t * 2 * TB;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -344,10 +347,14 @@ __global__ __launch_bounds__(256, PAD && D == 128 ? 1 : 2) void cross_dq_mfma_ke
           }
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            if ((t0 + t) * TILE + u * 32 + acc_row(r) < len) delta = fmaf(__builtin_amdgcn_exp2f(fmaf(s[r], c, -lse2)), dp[r], delta);
+            if (t * TILE + u * 32 + acc_row(r) < len) delta = fmaf(__builtin_amdgcn_exp2f(fmaf(s[r], c, -lse2)), dp[r], delta);
         }
       }
     delta += other_half(delta);
+    if (t0 > 0) {                                 // the part of the second tile alone
+      __syncthreads();
+      bring(0, 0);
+    }
   }
   if (lane < 32 && live && w.split == 0) a.delta[stat] = delta;
   f32x16 neg_delta, neg_lse;                      // the products start from these: dP less delta, scores less the log-sum-exp

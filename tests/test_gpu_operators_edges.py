@@ -247,6 +247,43 @@ def test_rows_that_are_not_finite_stay_among_what_they_meet(B, dtype, impl, sq, 
             assert torch.equal(t[others], c[others]), which
 
 
+@pytest.mark.parametrize("sq,heads,kv_heads,d,lens", [(4, 4, 2, 64, [3, 2500, 70, 128, 0]), (1, 8, 2, 128, [1, 3000, 100, 2]), (3, 2, 2, 80, [5, 2000, 127]),
+                                                      (130, 2, 2, 64, [3, 128, 65])])
+def test_gradients_of_queries_over_few_keys(B, sq, heads, kv_heads, d, lens):
+    """Samples of at most 128 keys, beside long ones that have the launch cut into parts and without: dQ has the roundings of dS and of
+    itself, none from the rounded context."""
+    rng = np.random.default_rng(sum(lens))
+    batch, sk, u = len(lens), max(lens), unit(1)
+    scale = d ** -0.5
+    q, k, v, g = (stored(rng.standard_normal((batch * rows, cols)) * mul, 1) for rows, cols, mul in
+                  ((sq, heads * d, 1.3), (sk, kv_heads * d, 1.0), (sk, kv_heads * d, 1.0), (sq, heads * d, 0.1)))
+    put = lambda t: torch.from_numpy(t).to(DEV).to(torch.bfloat16)
+    qd, kd, vd, gd = put(q), put(k), put(v), put(g)
+    n = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    ctx, dq, dk, dv, lse = torch.empty_like(qd), torch.empty_like(qd), torch.empty_like(kd), torch.empty_like(vd), torch.empty(batch, heads, sq, device=DEV)
+    B.bk_cross_attention_fwd(qd, kd, vd, ctx, lse, batch, heads, kv_heads, kv_len=n)
+    B.bk_cross_attention_bwd(qd, kd, vd, ctx, lse, gd, dq, dk, dv, batch, heads, kv_heads, kv_len=n)
+    want, bound = np.zeros(q.shape), np.zeros(q.shape)
+    for b, h, rq, rk, cq, ck in O._heads(q, k, v, batch, heads, kv_heads, lens):
+        m = rk.stop - rk.start
+        if m == 0 or m > 128:
+            bound[rq, cq] = np.inf if m else 0.0
+            continue
+        z = q[rq, cq] @ k[rk, ck].T * scale
+        p = np.exp(O.log_softmax(z))
+        gv, mags = g[rq, cq] @ v[rk, ck].T, np.abs(g[rq, cq]) @ np.abs(v[rk, ck]).T
+        delta = (p * gv).sum(1, keepdims=True)
+        ds = p * (gv - delta)
+        want[rq, cq] = scale * ds @ k[rk, ck]
+        # a probability: d products and sums of the score, its scale and exponent, the log-sum-exp's own sum of m terms
+        rel = E * ((d + 4) * (np.abs(q[rq, cq]) @ np.abs(k[rk, ck]).T) * scale + 8 * np.abs(z).max() + m + 16) * 2
+        b_delta = (p * (rel * np.abs(gv) + E * (d + 8) * mags)).sum(1, keepdims=True)
+        b_ds = p * (rel * np.abs(gv - delta) + b_delta + E * (d + 8) * (mags + np.abs(delta))) + u * np.abs(ds)
+        bound[rq, cq] = scale * (b_ds @ np.abs(k[rk, ck]) * (1 + 4 * u) + E * (m + 8) * (np.abs(ds) @ np.abs(k[rk, ck]))) + u * np.abs(want[rq, cq])
+    small = np.isfinite(bound).all(1)
+    within(host(dq)[small], want[small], bound[small] + 1e-38, "dq")
+
+
 # ---- rotary positions -------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", [0, 1])
